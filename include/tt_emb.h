@@ -251,6 +251,80 @@ int tt_emb_backward_update(tt_emb_t h, const float* grad_out, float lr, void* hi
  */
 int tt_emb_get_stats(tt_emb_t h, int64_t* U, int64_t* Q, int64_t* out_of_range);
 
+/* ---- plain tables beside the tensor-train one, and the norm of all gradients of a step ---- */
+
+enum { TT_EMB_FP32 = 0, TT_EMB_BF16 = 1, TT_EMB_FP16 = 2 };
+
+/* A row-major matrix in device memory, borrowed for the call; data aligned like one value. */
+typedef struct {
+  void* data;
+  int64_t rows;
+  int64_t ld;   /* values from the start of one row to the next, at least cols                     */
+  int32_t cols; /* 1 .. 65536                                                                       */
+  int32_t type; /* TT_EMB_FP32, TT_EMB_BF16 or TT_EMB_FP16                                          */
+} tt_emb_matrix;
+
+/*
+ * Lookup in a plain table (token vocabularies, node types, graphs too small to factorise):
+ *   out[b,:] = scale * table[ids[b],:]
+ * for the out->rows ids (below 2^30) of a batch, device int64; an id outside [0, table->rows) gives a zero row, as in
+ * tt_emb_forward.  table->rows below 2^31, table->cols = out->cols, any pair of types; products are formed in
+ * fp32 and rounded once.  out must not overlap the table.  May be captured into a HIP graph.
+ */
+int tt_emb_dense_forward(const tt_emb_matrix* table, const int64_t* ids, float scale, const tt_emb_matrix* out,
+                         void* hip_stream);
+
+/* Bytes of workspace that tt_emb_dense_backward needs for batches of up to max_batch (1 .. 2^30 - 1) rows. */
+int tt_emb_dense_workspace_bytes(int32_t cols, int64_t max_batch, size_t* bytes);
+
+/*
+ * Gradient of that lookup with respect to the table:
+ *   sum[v,:] = scale * (sum of grad[b,:] over the positions b with ids[b] = v),
+ * positions whose id is outside [0, dtable->rows) or equals padding_id (-1: no such id) taking no part.
+ *   add = 0   dtable[v,:] = sum[v,:]                 every row is written, zeros where no position has the id
+ *   add = 1   dtable[v,:] = dtable[v,:] + sum[v,:]   rows of ids in the batch only (gradients of several
+ *                                                    micro-batches; with the table itself as dtable and
+ *                                                    scale = -lr * s, a row-sparse SGD step)
+ * The sums are formed in fp32 in a fixed order (the same inputs give the same bits), rounded once.  ids: device
+ * int64[grad->rows].  grad->cols = dtable->cols, any pair of types; grad and dtable must not overlap.  workspace: device, 256-byte
+ * aligned, at least tt_emb_dense_workspace_bytes(grad->cols, grad->rows), else TT_EMB_ENOSPC; calls that share one must be
+ * ordered by a stream.  May be captured into a HIP graph.
+ */
+int tt_emb_dense_backward(const int64_t* ids, const tt_emb_matrix* grad, float scale, int64_t padding_id,
+                          const tt_emb_matrix* dtable, int add, void* workspace, size_t workspace_bytes,
+                          void* hip_stream);
+
+/* `count` values (0 .. 2^40) side by side in device memory, aligned like one value. */
+typedef struct {
+  void* data;
+  int64_t count;
+  int32_t type; /* TT_EMB_FP32, TT_EMB_BF16 or TT_EMB_FP16 */
+  int32_t unused;
+} tt_emb_values;
+
+/* Bytes of workspace that the two calls below need for n tensors. */
+int tt_emb_norm_workspace_bytes(int32_t n, size_t* bytes);
+
+/*
+ * 2-norm over all values of n tensors:  *norm = |scale| * sqrt(sum of squares),  device fp32.  Squares and sums are held
+ * in fp64, so that they neither overflow nor vanish, and added in a fixed order.  `in` is a host array, read during the
+ * call.  scale: what the values still have to be multiplied with (1 / the loss scale, 1 / micro-batches),
+ * finite.  n = 0 or no values: norm 0.  workspace: device, 256-byte aligned; calls that share one must be ordered by a
+ * stream.  May be captured into a HIP graph.
+ */
+int tt_emb_grad_norm(const tt_emb_values* in, int32_t n, float scale, float* norm, void* workspace,
+                     size_t workspace_bytes, void* hip_stream);
+
+/*
+ * The same norm, and the tensors scaled so that theirs is at most max_norm:
+ *   out[i] = in[i] * (scale * c),   c = min(1, max_norm / (*norm + eps)),
+ * formed in fp64, rounded to fp32 and then to the output's type.  out: tensors of the same counts and any types, or NULL for in place; an output may be
+ * its own input (same address and type) and overlaps no other.  In place with scale * c = 1 nothing is written.  A norm
+ * that is infinite or not a number is not hidden: c is 0 (and infinities become NaN) or NaN.  max_norm >= 0, eps >= 0.
+ */
+int tt_emb_grad_clip(const tt_emb_values* in, const tt_emb_values* out, int32_t n, float scale, float max_norm,
+                     float eps, float* norm, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /*
  * Per-kernel timing for benchmarks.  While enabled, every kernel launch is bracketed by a pair of
  * HIP events on the launch stream (this slows a step down; never enable it inside a throughput

@@ -25,6 +25,17 @@ class TTEmbConfig(ctypes.Structure):
                 ("device", c_int32), ("flags", c_uint32)]
 
 
+TT_EMB_FP32, TT_EMB_BF16, TT_EMB_FP16 = 0, 1, 2
+
+
+class TTEmbMatrix(ctypes.Structure):
+    _fields_ = [("data", c_void_p), ("rows", c_int64), ("ld", c_int64), ("cols", c_int32), ("type", c_int32)]
+
+
+class TTEmbValues(ctypes.Structure):
+    _fields_ = [("data", c_void_p), ("count", c_int64), ("type", c_int32), ("unused", c_int32)]
+
+
 class TTEmbError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -62,6 +73,15 @@ def load_library():
     lib.tt_emb_set_adam.argtypes = [c_void_p] + [c_void_p] * 6 + [c_float, c_float, c_float, c_int64]
     lib.tt_emb_prepare.argtypes = [c_void_p, c_void_p, c_int64, c_void_p]
     lib.tt_emb_get_stats.argtypes = [c_void_p, POINTER(c_int64), POINTER(c_int64), POINTER(c_int64)]
+    matp, valp = POINTER(TTEmbMatrix), POINTER(TTEmbValues)
+    lib.tt_emb_dense_forward.argtypes = [matp, c_void_p, c_float, matp, c_void_p]
+    lib.tt_emb_dense_workspace_bytes.argtypes = [c_int32, c_int64, POINTER(c_size_t)]
+    lib.tt_emb_dense_backward.argtypes = [c_void_p, matp, c_float, c_int64, matp, c_int, c_void_p, c_size_t,
+                                          c_void_p]
+    lib.tt_emb_norm_workspace_bytes.argtypes = [c_int32, POINTER(c_size_t)]
+    lib.tt_emb_grad_norm.argtypes = [valp, c_int32, c_float, c_void_p, c_void_p, c_size_t, c_void_p]
+    lib.tt_emb_grad_clip.argtypes = [valp, valp, c_int32, c_float, c_float, c_float, c_void_p, c_void_p, c_size_t,
+                                     c_void_p]
     lib.tt_emb_profile_enable.argtypes = [c_void_p, c_int]
     lib.tt_emb_profile_slots.argtypes = []
     lib.tt_emb_profile_read.argtypes = [c_void_p, c_int, POINTER(c_char_p), POINTER(c_int64),
@@ -74,6 +94,8 @@ def load_library():
     for name in ("tt_emb_workspace_bytes", "tt_emb_create", "tt_emb_forward", "tt_emb_prepare",
                  "tt_emb_backward_update", "tt_emb_forward_eval", "tt_emb_materialize", "tt_emb_lookup_static",
                  "tt_emb_set_reindex", "tt_emb_set_adagrad", "tt_emb_set_adam", "tt_emb_wait_backward", "tt_emb_get_stats", "tt_emb_profile_enable",
+                 "tt_emb_dense_forward", "tt_emb_dense_workspace_bytes", "tt_emb_dense_backward",
+                 "tt_emb_norm_workspace_bytes", "tt_emb_grad_norm", "tt_emb_grad_clip",
                  "tt_emb_profile_slots", "tt_emb_profile_read", "tt_emb_profile_peaks", "tt_emb_destroy"):
         getattr(lib, name).restype = c_int
     _lib = lib
@@ -189,7 +211,39 @@ def tt_emb_destroy(h) -> int:
     return load_library().tt_emb_destroy(h)
 
 
-# ---- convenience wrapper over torch tensors (memory and streams only)
+def tt_emb_dense_forward(table: TTEmbMatrix, ids_ptr: int, scale: float, out: TTEmbMatrix, stream: int) -> int:
+    return load_library().tt_emb_dense_forward(byref(table), ids_ptr, scale, byref(out), stream)
+
+
+def tt_emb_dense_workspace_bytes(cols: int, max_batch: int):
+    out = c_size_t(0)
+    rc = load_library().tt_emb_dense_workspace_bytes(cols, max_batch, byref(out))
+    return rc, int(out.value)
+
+
+def tt_emb_dense_backward(ids_ptr: int, grad: TTEmbMatrix, scale: float, padding_id: int, dtable: TTEmbMatrix,
+                          add: bool, ws_ptr: int, ws_bytes: int, stream: int) -> int:
+    return load_library().tt_emb_dense_backward(ids_ptr, byref(grad), scale, padding_id, byref(dtable),
+                                                1 if add else 0, ws_ptr, ws_bytes, stream)
+
+
+def tt_emb_norm_workspace_bytes(n: int):
+    out = c_size_t(0)
+    rc = load_library().tt_emb_norm_workspace_bytes(n, byref(out))
+    return rc, int(out.value)
+
+
+def tt_emb_grad_norm(values, n: int, scale: float, norm_ptr: int, ws_ptr: int, ws_bytes: int, stream: int) -> int:
+    """values: a ctypes array of n TTEmbValues (or None for n = 0), as in tt_emb_grad_clip."""
+    return load_library().tt_emb_grad_norm(values, n, scale, norm_ptr, ws_ptr, ws_bytes, stream)
+
+
+def tt_emb_grad_clip(values, out, n: int, scale: float, max_norm: float, eps: float, norm_ptr: int, ws_ptr: int,
+                     ws_bytes: int, stream: int) -> int:
+    return load_library().tt_emb_grad_clip(values, out, n, scale, max_norm, eps, norm_ptr, ws_ptr, ws_bytes, stream)
+
+
+# ---- convenience wrappers over torch tensors (memory and streams only)
 
 class TTEmbedding:
     """Owns the device tensors the library borrows: three cores and the workspace."""
@@ -368,3 +422,182 @@ class TTEmbedding:
             self.close()
         except Exception:
             pass
+
+
+def _type_of(t):
+    import torch
+    types = {torch.float32: TT_EMB_FP32, torch.bfloat16: TT_EMB_BF16, torch.float16: TT_EMB_FP16}
+    if t.dtype not in types:
+        raise ValueError(f"type {t.dtype}: float32, bfloat16 or float16 needed")
+    return types[t.dtype]
+
+
+class _OnDevice:
+    """Device, stream and workspace of the wrappers below."""
+
+    def __init__(self, device):
+        import torch
+        if device.type != "cuda":
+            raise ValueError(f"tensors on {device}: a GPU needed")
+        self.torch, self.device = torch, device
+
+    def _call(self, name, *args):
+        """The C function `name` with the current stream of this object's device as its last argument."""
+        torch = self.torch
+        stream = torch.cuda.current_stream(self.device).cuda_stream
+        if torch.cuda.current_device() == self.device.index:
+            rc = getattr(_lib, name)(*args, stream)
+        else:
+            with torch.cuda.device(self.device):
+                rc = getattr(_lib, name)(*args, stream)
+        if rc:
+            raise TTEmbError(rc, name)
+
+    def _make_workspace(self, nbytes):
+        self.workspace = self.torch.empty(nbytes + 256, dtype=self.torch.uint8, device=self.device)
+        self._ws_ptr = (self.workspace.data_ptr() + 255) & ~255
+        self.workspace_bytes = nbytes
+
+
+class DenseEmbedding(_OnDevice):
+    """A table kept as a plain matrix, beside tensor-train ones: lookup times a scale, and gradient.
+
+    weight: [rows, dim] on the GPU, float32, bfloat16 or float16, values of a row side by side (rows may lie further
+    apart); borrowed.  Ids outside the table give zero rows and no gradient; padding_id is an id that has a
+    row but no gradient.  Must not be used from two threads or streams at once (the workspace of backward)."""
+
+    def __init__(self, weight, max_batch: int, scale: float = 1.0, padding_id: int | None = None):
+        super().__init__(weight.device)
+        load_library()
+        self.weight, self.max_batch, self.scale = weight, int(max_batch), float(scale)
+        self.padding_id = -1 if padding_id is None else int(padding_id)
+        self._table = self._matrix(weight)
+        self.rows, self.dim = weight.shape
+        if self.dim < 1:
+            raise ValueError("rows without values")
+        rc, nbytes = tt_emb_dense_workspace_bytes(self.dim, self.max_batch)
+        if rc:
+            raise TTEmbError(rc, "tt_emb_dense_workspace_bytes")
+        self._make_workspace(nbytes)
+
+    def _matrix(self, t):
+        if t.dim() != 2 or t.device != self.device:
+            raise ValueError(f"matrix on {self.device} needed: shape {tuple(t.shape)} on {t.device}")
+        rows, cols = t.shape
+        step, side = t.stride()
+        if cols > 1 and side != 1 or rows > 1 and step < cols:
+            raise ValueError(f"strides {t.stride()}: values of a row side by side, rows that do not overlap needed")
+        return TTEmbMatrix(t.data_ptr(), rows, step if rows > 1 else cols, cols, _type_of(t))
+
+    def _ids(self, ids):
+        if ids.dtype != self.torch.int64 or ids.device != self.device or ids.dim() != 1 or not ids.is_contiguous():
+            raise ValueError("ids: contiguous int64 vector on the table's device needed")
+        if ids.numel() > self.max_batch:
+            raise TTEmbError(TT_EMB_ENOSPC, "DenseEmbedding")
+        return ids.data_ptr()
+
+    def _weight(self):
+        if self.weight.data_ptr() != self._table.data:  # the parameter's storage was replaced
+            self._table = self._matrix(self.weight)
+        return self._table
+
+    def forward(self, ids, out=None, dtype=None):
+        """scale * weight[ids], in the weight's type unless out or dtype says otherwise."""
+        ptr = self._ids(ids)
+        if out is None:
+            out = self.torch.empty((ids.numel(), self.dim), dtype=dtype or self.weight.dtype, device=self.device)
+        elif tuple(out.shape) != (ids.numel(), self.dim) or dtype not in (None, out.dtype):
+            raise ValueError(f"out: {(ids.numel(), self.dim)} of {dtype or out.dtype} needed, not {tuple(out.shape)}")
+        self._call("tt_emb_dense_forward", byref(self._weight()), ptr, self.scale, byref(self._matrix(out)))
+        return out
+
+    def backward(self, ids, grad_out, out=None, dtype=None, add: bool = False):
+        """Gradient of forward(ids) with respect to the weight, [rows, dim], for the upstream gradient grad_out.
+        With add, it is added to out, whose other rows are left alone."""
+        if out is None:
+            if add:
+                raise ValueError("add needs out")
+            out = self.torch.empty((self.rows, self.dim), dtype=dtype or self.weight.dtype, device=self.device)
+        elif tuple(out.shape) != (self.rows, self.dim) or dtype not in (None, out.dtype):
+            raise ValueError(f"out: {(self.rows, self.dim)} of {dtype or out.dtype} needed, not {tuple(out.shape)}")
+        self._backward(ids, grad_out, self.scale, self._matrix(out), add)
+        return out
+
+    def backward_update(self, ids, grad_out, lr: float):
+        """SGD step of the weight's rows that ids name: weight -= lr * gradient, rounded to the weight's type."""
+        self._backward(ids, grad_out, -float(lr) * self.scale, self._weight(), True)
+
+    def _backward(self, ids, grad_out, scale, target, add):
+        ptr = self._ids(ids)
+        if tuple(grad_out.shape) != (ids.numel(), self.dim):
+            raise ValueError(f"grad_out: {(ids.numel(), self.dim)} needed, not {tuple(grad_out.shape)}")
+        self._call("tt_emb_dense_backward", ptr, byref(self._matrix(grad_out)), scale, self.padding_id, byref(target),
+                   1 if add else 0, self._ws_ptr, self.workspace_bytes)
+
+
+class GradientClip(_OnDevice):
+    """The 2-norm over all values of many tensors, and the tensors scaled to a largest norm.
+
+    tensors: on one GPU, float32, bfloat16 or float16, each without gaps (any order of dimensions), not overlapping
+    each other; borrowed.  out: tensors of the same sizes, in any of the types, that receive the scaled
+    values; None: in place.  Must not be used from two threads or streams at once."""
+
+    def __init__(self, tensors, out=None):
+        self.tensors = list(tensors)
+        if not self.tensors:
+            raise ValueError("no tensors")
+        super().__init__(self.tensors[0].device)
+        load_library()
+        self._in = self._values(self.tensors)
+        self.out, self._out = None, None
+        if out is not None:
+            self.out = list(out)
+            if [t.shape for t in self.out] != [t.shape for t in self.tensors]:
+                raise ValueError("out: tensors of the same shapes needed")
+            if any(a.stride() != b.stride() for a, b in zip(self.tensors, self.out) if a.numel() > 1):
+                raise ValueError("out: tensors of the same strides needed")
+            self._out = self._values(self.out)
+        rc, nbytes = tt_emb_norm_workspace_bytes(len(self.tensors))
+        if rc:
+            raise TTEmbError(rc, "tt_emb_norm_workspace_bytes")
+        self._make_workspace(nbytes)
+
+    def _values(self, tensors):
+        values = (TTEmbValues * len(tensors))()
+        for v, t in zip(values, tensors):
+            if t.device != self.device:
+                raise ValueError(f"tensor on {t.device}, not {self.device}")
+            if not (t.is_contiguous() or self._dense(t)):
+                raise ValueError(f"tensor of shape {tuple(t.shape)} and strides {t.stride()} has gaps or overlaps")
+            v.data, v.count, v.type = t.data_ptr(), t.numel(), _type_of(t)
+        return values
+
+    @staticmethod
+    def _dense(t):
+        size = 1
+        for step, n in sorted((s, n) for s, n in zip(t.stride(), t.shape) if n > 1):
+            if step != size:
+                return False
+            size *= n
+        return True
+
+    def _norm(self, out):
+        if out is None:
+            return self.torch.empty((), dtype=self.torch.float32, device=self.device)
+        if out.numel() != 1 or out.dtype != self.torch.float32 or out.device != self.device:
+            raise ValueError("out: one float32 on the tensors' device needed")
+        return out
+
+    def norm(self, scale: float = 1.0, out=None):
+        """|scale| * the norm, as a float32 on the device."""
+        out = self._norm(out)
+        self._call("tt_emb_grad_norm", self._in, len(self._in), float(scale), out.data_ptr(), self._ws_ptr,
+                   self.workspace_bytes)
+        return out
+
+    def clip(self, max_norm: float, scale: float = 1.0, eps: float = 1e-6, out=None):
+        """Scales the tensors by scale and down to max_norm; returns the norm before, |scale| included."""
+        out = self._norm(out)
+        self._call("tt_emb_grad_clip", self._in, self._out, len(self._in), float(scale), float(max_norm), float(eps),
+                   out.data_ptr(), self._ws_ptr, self.workspace_bytes)
+        return out

@@ -74,6 +74,22 @@ void launch_direct_apply(const Plan&, const DirectBuffers&, int B, float* g1, fl
 bool table_streamed(const Plan&, int64_t count);
 void launch_table(const Plan&, const float* g1, const float* g2, const float* g3, int64_t first,
                   int64_t count, float* out, hipStream_t);
+// plain tables (tt_emb_dense.hip)
+void launch_table_sort_pass(const Workspace&, const SortKeys&, const TableSource&, int B, int pass, hipStream_t,
+                            int which);
+void launch_dense_rows(const tt_emb_matrix& table, const int64_t* ids, int B, float scale, const tt_emb_matrix& out,
+                       hipStream_t);
+void launch_dense_zero(const tt_emb_matrix& out, hipStream_t);
+void launch_dense_sum(const DenseWork&, int sorted, int B, const tt_emb_matrix& grad, float scale,
+                      const tt_emb_matrix& out, bool add, hipStream_t);
+void launch_dense_join(const DenseWork&, int sorted, int B, float scale, const tt_emb_matrix& out, bool add,
+                       hipStream_t);
+// norm and clipping of many tensors (tt_emb_clip.hip)
+int64_t clip_units(int64_t count);
+int launch_norm_parts(const ClipList&, double* parts, hipStream_t);
+void launch_norm_total(const double* parts, int n, float scale, float max_norm, float eps, float* norm, double* factor,
+                       hipStream_t);
+void launch_clip(const ClipList&, const double* factor, hipStream_t);
 hipError_t calibrate(void* buf, size_t bytes, hipStream_t, double* copy_bytes_per_s,
                      double* mfma_flops_per_s, double* gather_bytes_per_s,
                      double* far_gather_bytes_per_s);
@@ -83,7 +99,7 @@ static const char* const kSlotNames[kSlotCount] = {
     "prefix_fwd", "row_fwd",  "gsum",         "gsum_fix",  "u_bwd",      "dg3",        "prefix_bwd",
     "sgd",        "direct_fwd", "direct_bwd", "direct_apply", "table", "lookup", "event_pair"};
 
-static thread_local std::string g_hip_error = "HIP call failed";
+static thread_local char g_hip_error[256] = "HIP call failed";  // no allocation on the way out of a failure
 
 static inline int64_t cdiv64(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
@@ -361,7 +377,7 @@ static IdSource id_source(const tt_emb* h, const int64_t* ids, int64_t base, boo
 }
 
 static int hip_fail(hipError_t e) {
-  g_hip_error = std::string("HIP: ") + hipGetErrorString(e);
+  std::snprintf(g_hip_error, sizeof(g_hip_error), "HIP: %s", hipGetErrorString(e));
   return TT_EMB_EHIP;
 }
 
@@ -959,6 +975,97 @@ static int backward_indexed(tt_emb* h, const float* grad_out, float lr, int B, h
                   [&] { launch_sgd(pl, ws, h->g1, h->g2, h->g3, lr, h->ada, stop, st); });
 }
 
+// ---- plain tables, norm and clipping ----
+
+static bool known_type(int type) { return type == TT_EMB_FP32 || type == TT_EMB_BF16 || type == TT_EMB_FP16; }
+static size_t type_bytes(int type) { return type == TT_EMB_FP32 ? 4 : 2; }
+constexpr int kDenseCols = 1 << 16;  // widest row
+constexpr int64_t kDenseBatch = int64_t(1) << 30;
+
+static bool good_matrix(const tt_emb_matrix* m, int64_t most_rows) {
+  return m != nullptr && known_type(m->type) && m->rows >= 0 && m->rows < most_rows && m->cols >= 1 &&
+         m->cols <= kDenseCols && m->ld >= m->cols && m->ld <= (int64_t(1) << 40) &&
+         (m->rows == 0 || m->data != nullptr) && ((uintptr_t)m->data & (type_bytes(m->type) - 1)) == 0;
+}
+static bool good_ids(const int64_t* ids, int64_t B) { return B == 0 || (ids != nullptr && ((uintptr_t)ids & 7u) == 0); }
+
+static size_t carve_dense(int cols, int64_t max_batch, char* base, DenseWork* ws) {
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    char* p = base + off;
+    off += (bytes + 255) & ~(size_t)255;
+    return p;
+  };
+  const size_t mB = (size_t)max_batch, tiles = (mB + kDenseTile - 1) / kDenseTile;
+  const int stride = (cols + 3) & ~3;
+  DenseWork w{};
+  w.sort.ctr = (Counters*)take(sizeof(Counters));
+  for (int k = 0; k < 2; ++k) {
+    w.sort.key[k] = (uint32_t*)take(mB * 4);
+    w.sort.val[k] = (uint32_t*)take(mB * 4);
+  }
+  w.sort.cnt = (uint32_t*)take((size_t)sort_blocks_most(max_batch) * kMaxBins * 4);
+  w.sort.tot = (uint32_t*)take(kMaxBins * 4);
+  w.head = (float*)take(tiles * stride * 4);
+  w.tail = (float*)take(tiles * stride * 4);
+  w.stride = stride;
+  if (ws != nullptr) *ws = w;
+  return off;
+}
+
+// Packs the tensors that hold anything into launches' lists, and calls f with each.  out: where they go, or null.
+template <class F>
+static void clip_lists(const tt_emb_values* in, const tt_emb_values* out, int n, F&& f) {
+  ClipList list;
+  list.n = 0;
+  list.units = 0;
+  for (int i = 0; i < n; ++i) {
+    if (in[i].count == 0) continue;
+    const tt_emb_values& to = out != nullptr ? out[i] : in[i];
+    list.item[list.n++] = ClipItem{in[i].data, to.data, in[i].count, list.units, in[i].type, to.type};
+    list.units += clip_units(in[i].count);
+    if (list.n == kClipItems) {
+      f(list);
+      list.n = 0;
+      list.units = 0;
+    }
+  }
+  if (list.n > 0) f(list);
+}
+
+static bool good_values(const tt_emb_values* v, int n) {
+  if (n < 0 || (n > 0 && v == nullptr)) return false;
+  for (int i = 0; i < n; ++i)
+    if (!known_type(v[i].type) || v[i].count < 0 || v[i].count > (int64_t(1) << 40) ||
+        (v[i].count > 0 && v[i].data == nullptr) || ((uintptr_t)v[i].data & (type_bytes(v[i].type) - 1)) != 0)
+      return false;
+  return true;
+}
+
+static size_t norm_bytes(int n) {  // partial sums of every launch, and the factor behind them
+  const int64_t launches = std::max<int64_t>(cdiv64(n, kClipItems), 1);
+  return (size_t)launches * kClipBlocks * sizeof(double) + 256;
+}
+
+// Both steps of the norm; factor: also what clipping multiplies with.
+static int run_norm(const tt_emb_values* in, int n, float scale, float max_norm, float eps, float* norm, void* workspace,
+                    double* factor, hipStream_t st) {
+  double* parts = (double*)workspace;
+  int made = 0;
+  clip_lists(in, nullptr, n, [&](const ClipList& list) { made += launch_norm_parts(list, parts + made, st); });
+  launch_norm_total(parts, made, scale, max_norm, eps, norm, factor, st);
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? TT_EMB_OK : hip_fail(e);
+}
+
+static int check_norm(const tt_emb_values* in, int n, float scale, const float* norm, const void* workspace,
+                      size_t workspace_bytes) {
+  if (!good_values(in, n) || !std::isfinite(scale) || norm == nullptr || ((uintptr_t)norm & 3u) != 0 ||
+      workspace == nullptr || ((uintptr_t)workspace & 255u) != 0)
+    return TT_EMB_EINVAL;
+  return workspace_bytes < norm_bytes(n) ? TT_EMB_ENOSPC : TT_EMB_OK;
+}
+
 extern "C" {
 
 int tt_emb_backward_update(tt_emb_t h, const float* grad_out, float lr, void* hip_stream) {
@@ -1123,13 +1230,95 @@ int tt_emb_destroy(tt_emb_t h) {
   return TT_EMB_OK;
 }
 
+int tt_emb_dense_forward(const tt_emb_matrix* table, const int64_t* ids, float scale, const tt_emb_matrix* out,
+                         void* hip_stream) {
+  if (!good_matrix(table, int64_t(1) << 31) || !good_matrix(out, kDenseBatch) || table->cols != out->cols ||
+      !good_ids(ids, out->rows))
+    return TT_EMB_EINVAL;
+  if (out->rows == 0) return TT_EMB_OK;
+  launch_dense_rows(*table, ids, (int)out->rows, scale, *out, (hipStream_t)hip_stream);
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? TT_EMB_OK : hip_fail(e);
+}
+
+int tt_emb_dense_workspace_bytes(int32_t cols, int64_t max_batch, size_t* bytes) {
+  if (bytes == nullptr || cols < 1 || cols > kDenseCols || max_batch < 1 || max_batch >= kDenseBatch)
+    return TT_EMB_EINVAL;
+  *bytes = carve_dense(cols, max_batch, nullptr, nullptr);
+  return TT_EMB_OK;
+}
+
+int tt_emb_dense_backward(const int64_t* ids, const tt_emb_matrix* grad, float scale, int64_t padding_id,
+                          const tt_emb_matrix* dtable, int add, void* workspace, size_t workspace_bytes,
+                          void* hip_stream) {
+  if (!good_matrix(grad, kDenseBatch) || !good_matrix(dtable, int64_t(1) << 31) || grad->cols != dtable->cols ||
+      !good_ids(ids, grad->rows))
+    return TT_EMB_EINVAL;
+  const int B = (int)grad->rows;
+  hipStream_t st = (hipStream_t)hip_stream;
+  if (B > 0) {
+    if (workspace == nullptr || ((uintptr_t)workspace & 255u) != 0) return TT_EMB_EINVAL;
+    if (workspace_bytes < carve_dense(grad->cols, B, nullptr, nullptr)) return TT_EMB_ENOSPC;
+  }
+  if (dtable->rows == 0) return TT_EMB_OK;
+  if (!add) launch_dense_zero(*dtable, st);
+  if (B > 0) {
+    DenseWork ws;
+    carve_dense(grad->cols, B, (char*)workspace, &ws);
+    const SortKeys sk = sort_keys((uint32_t)dtable->rows, 0);
+    const TableSource src{ids, dtable->rows, padding_id};
+    for (int pass = 0; pass < sk.passes; ++pass) {
+      launch_table_sort_pass(ws.sort, sk, src, B, pass, st, 0);
+      if (!sort_folds(sk, B, pass, false)) launch_table_sort_pass(ws.sort, sk, src, B, pass, st, 2);
+      launch_table_sort_pass(ws.sort, sk, src, B, pass, st, 1);
+    }
+    launch_dense_sum(ws, sk.sorted(), B, *grad, scale, *dtable, add != 0, st);
+    // a run that needs joining covers a whole tile besides those that it starts and ends in
+    if (B > 2 * kDenseTile) launch_dense_join(ws, sk.sorted(), B, scale, *dtable, add != 0, st);
+  }
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? TT_EMB_OK : hip_fail(e);
+}
+
+int tt_emb_norm_workspace_bytes(int32_t n, size_t* bytes) {
+  if (bytes == nullptr || n < 0) return TT_EMB_EINVAL;
+  *bytes = norm_bytes(n);
+  return TT_EMB_OK;
+}
+
+int tt_emb_grad_norm(const tt_emb_values* in, int32_t n, float scale, float* norm, void* workspace,
+                     size_t workspace_bytes, void* hip_stream) {
+  const int rc = check_norm(in, n, scale, norm, workspace, workspace_bytes);
+  if (rc != TT_EMB_OK) return rc;
+  return run_norm(in, n, scale, 0.f, 0.f, norm, workspace, nullptr, (hipStream_t)hip_stream);
+}
+
+int tt_emb_grad_clip(const tt_emb_values* in, const tt_emb_values* out, int32_t n, float scale, float max_norm,
+                     float eps, float* norm, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  int rc = check_norm(in, n, scale, norm, workspace, workspace_bytes);
+  if (rc != TT_EMB_OK) return rc;
+  if (!(max_norm >= 0.f) || !(eps >= 0.f)) return TT_EMB_EINVAL;
+  if (out != nullptr) {
+    if (!good_values(out, n)) return TT_EMB_EINVAL;
+    for (int i = 0; i < n; ++i)
+      if (out[i].count != in[i].count) return TT_EMB_EINVAL;
+  }
+  hipStream_t st = (hipStream_t)hip_stream;
+  double* factor = (double*)((char*)workspace + norm_bytes(n) - 256);
+  rc = run_norm(in, n, scale, max_norm, eps, norm, workspace, factor, st);
+  if (rc != TT_EMB_OK) return rc;
+  clip_lists(in, out, n, [&](const ClipList& list) { launch_clip(list, factor, st); });
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? TT_EMB_OK : hip_fail(e);
+}
+
 const char* tt_emb_strerror(int code) {
   switch (code) {
     case TT_EMB_OK: return "ok";
     case TT_EMB_EINVAL: return "invalid argument (null pointer, non-positive or unsupported size)";
     case TT_EMB_ENOSPC: return "batch larger than max_batch, or workspace too small";
     case TT_EMB_ESTATE: return "the handle's state does not allow this call (no pending forward, a pending forward, or a capture on a handle that has prepared)";
-    case TT_EMB_EHIP: return g_hip_error.c_str();
+    case TT_EMB_EHIP: return g_hip_error;
     case TT_EMB_ERANGE: return "an id of the last batch was outside [0, N)";
     case TT_EMB_EINTERNAL: return "internal error: a kernel met an impossible index";
     default: return "unknown error code";

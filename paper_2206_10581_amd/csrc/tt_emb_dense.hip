@@ -1,0 +1,319 @@
+// Plain embedding tables beside the tensor-train one: rows by id times a scale, and the table's gradient as
+// sums over the positions of each id, found by a stable sort of the ids.  fp32, bf16 and fp16; products and sums
+// in fp32, rounded once where a value is stored.
+#include <type_traits>
+
+#include "tt_emb_internal.h"
+
+namespace ttemb {
+
+constexpr int kDenseThreads = 256;
+
+// Values that a thread takes at once: 16 bytes of the type that is read.  VEC = 1: rows shorter than that.
+// Rows start wherever their strides put them, so these vectors are aligned like single values.
+template <class T, int VEC>
+struct Piece {
+  typedef T V __attribute__((ext_vector_type(VEC), aligned(sizeof(T))));
+};
+template <class T>
+struct Piece<T, 1> {
+  typedef T V;
+};
+
+template <int VEC, class T>
+__device__ __forceinline__ void load_piece(const T* p, float (&x)[VEC]) {
+  const typename Piece<T, VEC>::V v = *(const typename Piece<T, VEC>::V*)p;
+  if constexpr (VEC == 1) {
+    x[0] = (float)v;
+  } else {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) x[i] = (float)v[i];
+  }
+}
+
+template <int VEC, class T>
+__device__ __forceinline__ void store_piece(T* p, const float (&x)[VEC]) {
+  typename Piece<T, VEC>::V v;
+  if constexpr (VEC == 1) {
+    v = (T)x[0];
+  } else {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) v[i] = (T)x[i];
+  }
+  *(typename Piece<T, VEC>::V*)p = v;
+}
+
+// How a block's threads are dealt: 2^lanes of them side by side along a row, blockIdx.y over what is left of it.
+struct Lanes {
+  int lanes;   // log2
+  int pieces;  // of a row
+};
+
+// The last piece of a row that is no multiple of VEC starts early and holds some values of its neighbour again.
+template <int VEC>
+__device__ __forceinline__ int piece_start(int c, int cols) {
+  return min(c * VEC, cols - VEC);
+}
+
+// out[b] = scale * W[ids[b]], zeros for ids outside the table
+template <class TI, class TO, int VEC>
+__global__ __launch_bounds__(kDenseThreads) void k_dense_rows(const TI* __restrict__ table, int64_t ld, int64_t rows,
+                                                              const int64_t* __restrict__ ids, int B, float scale,
+                                                              TO* __restrict__ out, int64_t ld_out, int cols, Lanes ln) {
+  const int c = (blockIdx.y << ln.lanes) + (threadIdx.x & ((1 << ln.lanes) - 1));
+  if (c >= ln.pieces) return;
+  const int col = piece_start<VEC>(c, cols), step = gridDim.x * (kDenseThreads >> ln.lanes);
+  for (int b = blockIdx.x * (kDenseThreads >> ln.lanes) + (threadIdx.x >> ln.lanes); b < B; b += step) {
+    const int64_t id = ids[b];
+    float x[VEC];
+    if ((uint64_t)id < (uint64_t)rows) {
+      load_piece<VEC>(table + id * ld + col, x);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) x[i] *= scale;
+    } else {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) x[i] = 0.f;
+    }
+    store_piece<VEC>(out + b * ld_out + col, x);
+  }
+}
+
+template <class TO, int VEC>
+__global__ __launch_bounds__(kDenseThreads) void k_dense_zero(TO* __restrict__ out, int64_t ld, int64_t rows, int cols,
+                                                              Lanes ln) {
+  const int c = (blockIdx.y << ln.lanes) + (threadIdx.x & ((1 << ln.lanes) - 1));
+  if (c >= ln.pieces) return;
+  const int col = piece_start<VEC>(c, cols), step = gridDim.x * (kDenseThreads >> ln.lanes);
+  const float zero[VEC] = {};
+  for (int64_t v = blockIdx.x * (kDenseThreads >> ln.lanes) + (threadIdx.x >> ln.lanes); v < rows; v += step)
+    store_piece<VEC>(out + v * ld + col, zero);
+}
+
+// How tile t of the sorted slots takes part in the runs that cross its borders.  A run that starts in a tile is
+// summed by it alone if it ends in the next tile at the latest.  A longer one is cut at the borders of the tiles:
+// the first tile's part goes to `tail`, every other's to `head`, and k_dense_join adds them up.
+struct TileRuns {
+  int s0, s1;        // slots of the tile
+  int limit;         // end of the slots that the tile adds up, beyond s1 where its last run goes on
+  uint32_t first, last;  // ids of its first and last slot
+  bool began;        // the first slot's run began in an earlier tile
+  bool head;         // and is a long one: the tile leaves its part
+  bool tail;         // the last run begins here and is a long one
+  __device__ __forceinline__ TileRuns(const uint32_t* __restrict__ key, int t, int B, uint32_t none) {
+    s0 = t * kDenseTile;
+    s1 = min(s0 + kDenseTile, B);
+    first = key[s0];
+    last = key[s1 - 1];
+    const bool more = s1 < B;
+    const uint32_t next = more ? key[s1] : none;
+    const uint32_t after = more && s1 + kDenseTile < B ? key[s1 + kDenseTile] : none;
+    began = s0 > 0 && key[max(s0 - 1, 0)] == first;
+    head = began && first < none &&
+           ((t >= 2 && key[max(s0 - kDenseTile - 1, 0)] == first) || next == first);
+    const bool goes_on = last < none && next == last && !(began && first == last);
+    tail = goes_on && after == last;
+    limit = goes_on && !tail ? min(s1 + kDenseTile, B) : s1;
+  }
+};
+
+template <class TO, int VEC, bool ADD>
+__device__ __forceinline__ void put_sum(TO* __restrict__ row, int col, int c, float scale, const float (&sum)[VEC]) {
+  float x[VEC];
+  if constexpr (!ADD) {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) x[i] = scale * sum[i];
+    store_piece<VEC>(row + col, x);
+  } else if (col == c * VEC) {
+    load_piece<VEC>(row + col, x);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) x[i] = fmaf(scale, sum[i], x[i]);
+    store_piece<VEC>(row + col, x);
+  } else {  // values that the neighbour has too are its own to add
+    for (int i = c * VEC - col; i < VEC; ++i) {
+      float s = 0.f;  // sum[i], with constant indexes
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) s = k == i ? sum[k] : s;
+      row[col + i] = (TO)fmaf(scale, s, (float)row[col + i]);
+    }
+  }
+}
+
+// Sums of the gradient rows of every id whose run of sorted slots a tile owns.
+template <class TI, class TO, int VEC, bool ADD>
+__global__ __launch_bounds__(kDenseThreads) void k_dense_sum(const uint32_t* __restrict__ key,
+                                                             const uint32_t* __restrict__ pos, int B, uint32_t none,
+                                                             const TI* __restrict__ grad, int64_t ld_grad, int cols,
+                                                             Lanes ln, float scale, TO* __restrict__ out, int64_t ld,
+                                                             float* __restrict__ head, float* __restrict__ tail,
+                                                             int stride) {
+  constexpr int kAhead = 8;
+  const int c = (blockIdx.y << ln.lanes) + (threadIdx.x & ((1 << ln.lanes) - 1));
+  if (c >= ln.pieces) return;
+  const int col = piece_start<VEC>(c, cols), step = gridDim.x * (kDenseThreads >> ln.lanes);
+  const int tiles = (B + kDenseTile - 1) / kDenseTile;
+  for (int t = blockIdx.x * (kDenseThreads >> ln.lanes) + (threadIdx.x >> ln.lanes); t < tiles; t += step) {
+    const TileRuns r(key, t, B, none);
+    if (r.first >= none) return;  // positions without an id are last
+    uint32_t cur = none;
+    float acc[VEC];
+    auto flush = [&](bool at_end) {
+      if (cur >= none) return;
+      if (r.began && cur == r.first) {
+        store_piece<VEC>(head + (size_t)t * stride + col, acc);
+      } else if (at_end && r.tail) {
+        store_piece<VEC>(tail + (size_t)t * stride + col, acc);
+      } else {
+        put_sum<TO, VEC, ADD>(out + (int64_t)cur * ld, col, c, scale, acc);
+      }
+    };
+    for (int s = r.s0; s < r.limit; s += kAhead) {
+      uint32_t k[kAhead];
+      float x[kAhead][VEC];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const int at = min(s + i, B - 1);
+        k[i] = key[at];
+        const bool mine = s + i < r.limit && (s + i < r.s1 || k[i] == r.last) && !(r.began && !r.head && k[i] == r.first);
+        k[i] = mine ? k[i] : none;
+        if (k[i] < none) load_piece<VEC>(grad + pos[at] * ld_grad + col, x[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        if (k[i] >= none) continue;
+        if (k[i] != cur) {
+          flush(false);
+          cur = k[i];
+#pragma unroll
+          for (int j = 0; j < VEC; ++j) acc[j] = 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) acc[j] += x[i][j];
+      }
+    }
+    flush(true);
+  }
+}
+
+// Long runs: the parts that their tiles left, in order.
+template <class TO, bool ADD>
+__global__ __launch_bounds__(kDenseThreads) void k_dense_join(const uint32_t* __restrict__ key, int B, uint32_t none,
+                                                              int cols, float scale, TO* __restrict__ out, int64_t ld,
+                                                              const float* __restrict__ head,
+                                                              const float* __restrict__ tail, int stride) {
+  const int tiles = (B + kDenseTile - 1) / kDenseTile;
+  const int col = blockIdx.y * kDenseThreads + threadIdx.x;
+  for (int t = blockIdx.x; t < tiles; t += gridDim.x) {
+    const TileRuns r(key, t, B, none);
+    if (r.first >= none) return;
+    if (!r.tail || col >= cols) continue;
+    int lo = t + 2, hi = tiles;  // the run covers the first slots of tiles t+1 .. lo-1 at least, never that of hi
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if (key[mid * kDenseTile] == r.last) lo = mid + 1;
+      else hi = mid;
+    }
+    float sum[1] = {tail[(size_t)t * stride + col]};
+#pragma unroll 8
+    for (int j = t + 1; j < lo; ++j) sum[0] += head[(size_t)j * stride + col];
+    put_sum<TO, 1, ADD>(out + (int64_t)r.last * ld, col, col, scale, sum);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// host-side launchers
+
+template <class F>
+static void with_type(int type, F&& f) {
+  switch (type) {
+    case TT_EMB_BF16: f(__bf16{}); break;
+    case TT_EMB_FP16: f(_Float16{}); break;
+    default: f(float{}); break;
+  }
+}
+
+// f gets the number of values of a piece: 16 bytes of a type, or one where the rows are shorter
+template <class T, class F>
+static void with_piece(int cols, F&& f) {
+  constexpr int kVec = 16 / (int)sizeof(T);
+  if (cols >= kVec) f(std::integral_constant<int, kVec>{});
+  else f(std::integral_constant<int, 1>{});
+}
+
+static Lanes lanes_of(int cols, int vec) {
+  Lanes ln{0, (cols + vec - 1) / vec};
+  while ((1 << ln.lanes) < ln.pieces && (1 << ln.lanes) < kDenseThreads) ++ln.lanes;
+  return ln;
+}
+
+// Blocks for `rows` rows (or tiles) dealt like this; kernels stride over what a grid of 2^22 blocks leaves.
+static dim3 grid_of(int64_t rows, const Lanes& ln) {
+  const int64_t per = kDenseThreads >> ln.lanes, y = ((ln.pieces - 1) >> ln.lanes) + 1;
+  const int64_t x = std::min<int64_t>((rows + per - 1) / per, (int64_t)(1 << 22) / y);
+  return dim3((unsigned)x, (unsigned)y);
+}
+
+void launch_dense_rows(const tt_emb_matrix& table, const int64_t* ids, int B, float scale, const tt_emb_matrix& out,
+                       hipStream_t st) {
+  with_type(table.type, [&](auto ti) {
+    with_type(out.type, [&](auto to) {
+      using TI = decltype(ti);
+      using TO = decltype(to);
+      with_piece<TI>(table.cols, [&](auto vec) {
+        const Lanes ln = lanes_of(table.cols, vec());
+        k_dense_rows<TI, TO, vec()><<<grid_of(B, ln), kDenseThreads, 0, st>>>(
+            (const TI*)table.data, table.ld, table.rows, ids, B, scale, (TO*)out.data, out.ld, table.cols, ln);
+      });
+    });
+  });
+}
+
+void launch_dense_zero(const tt_emb_matrix& out, hipStream_t st) {
+  with_type(out.type, [&](auto to) {
+    using TO = decltype(to);
+    with_piece<TO>(out.cols, [&](auto vec) {
+      const Lanes ln = lanes_of(out.cols, vec());
+      k_dense_zero<TO, vec()><<<grid_of(out.rows, ln), kDenseThreads, 0, st>>>((TO*)out.data, out.ld, out.rows,
+                                                                              out.cols, ln);
+    });
+  });
+}
+
+void launch_dense_sum(const DenseWork& ws, int sorted, int B, const tt_emb_matrix& grad, float scale,
+                      const tt_emb_matrix& out, bool add, hipStream_t st) {
+  const uint32_t none = (uint32_t)out.rows;
+  const int64_t tiles = (B + kDenseTile - 1) / kDenseTile;
+  with_type(grad.type, [&](auto ti) {
+    with_type(out.type, [&](auto to) {
+      using TI = decltype(ti);
+      using TO = decltype(to);
+      with_piece<TI>(grad.cols, [&](auto vec) {
+        const Lanes ln = lanes_of(grad.cols, vec());
+        auto launch = [&](auto kernel) {
+          kernel<<<grid_of(tiles, ln), kDenseThreads, 0, st>>>(ws.sort.key[sorted], ws.sort.val[sorted], B, none,
+                                                               (const TI*)grad.data, grad.ld, grad.cols, ln, scale,
+                                                               (TO*)out.data, out.ld, ws.head, ws.tail, ws.stride);
+        };
+        if (add) launch(k_dense_sum<TI, TO, vec(), true>);
+        else launch(k_dense_sum<TI, TO, vec(), false>);
+      });
+    });
+  });
+}
+
+void launch_dense_join(const DenseWork& ws, int sorted, int B, float scale, const tt_emb_matrix& out, bool add,
+                       hipStream_t st) {
+  const uint32_t none = (uint32_t)out.rows;
+  const int tiles = (B + kDenseTile - 1) / kDenseTile;
+  with_type(out.type, [&](auto to) {
+    using TO = decltype(to);
+    const dim3 grid((unsigned)std::min(tiles, 1 << 14), (unsigned)(out.cols + kDenseThreads - 1) / kDenseThreads);
+    auto launch = [&](auto kernel) {
+      kernel<<<grid, kDenseThreads, 0, st>>>(ws.sort.key[sorted], B, none, out.cols, scale, (TO*)out.data, out.ld,
+                                             ws.head, ws.tail, ws.stride);
+    };
+    if (add) launch(k_dense_join<TO, true>);
+    else launch(k_dense_join<TO, false>);
+  });
+}
+
+}  // namespace ttemb

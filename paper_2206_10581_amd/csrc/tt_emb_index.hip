@@ -776,11 +776,10 @@ __global__ __launch_bounds__(NT) void k_group(
 
 static inline int cdiv(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
-// One of the three kernels of a pass.  clear: the first one also clears the tables that the steps
-// behind the sort add into (lookups have none).
-template <int NT>
-static void sort_pass(const Plan& pl, const Workspace& ws, const SortKeys& sk, const IdSource& src, int B,
-                      int pass, bool beside, bool clear, hipStream_t st, int which) {
+// One of the three kernels of a pass.  first: launches the histogram of the first pass, which reads the ids.
+template <int NT, class FIRST>
+static void sort_pass(const Workspace& ws, const SortKeys& sk, int B, int pass, bool beside, hipStream_t st,
+                      int which, FIRST&& first) {
   const int blocks = cdiv(B, sort_items(NT));
   const int shift = sk.low + pass * sk.per;
   const int bits = sk.bits_of(pass);
@@ -791,18 +790,11 @@ static void sort_pass(const Plan& pl, const Workspace& ws, const SortKeys& sk, c
     k_sort_colscan<<<cdiv(1 << bits, kScanBins), kScanThreads, 0, st>>>(ws.cnt, ws.tot, blocks,
                                                                        1 << bits);
   } else if (which == 0) {
-    auto first = [&](auto from) {
-      k_sort_hist<NT><<<blocks, NT, 0, st>>>(
-          from, kin, B, sk.sentinel, shift, bits, folds, ws.cnt, (uint32_t*)ws.g1_first,
-          clear ? 2 * (int)pl.sh.n1 : 0, ws.ctr);
-    };
     if (pass > 0)
       k_sort_hist<NT><<<blocks, NT, 0, st>>>(KeysInPlace{}, kin, B, sk.sentinel, shift, bits, folds, ws.cnt, nullptr, 0,
                                              ws.ctr);
-    else if (sk.low > 0)  // by prefix
-      first(PrefixSource{src, sk.low, pl.user_n1, pl.sh.n2, pl.sh.n3});
     else
-      first(src);
+      first(blocks, kin, shift, bits, folds);
   } else {
     auto scatter = [&](auto kernel, auto ops) { kernel<<<blocks, NT, 0, st>>>(ops, B, bits, ws.cnt, ws.tot); };
     if (pass == 0) {
@@ -815,14 +807,42 @@ static void sort_pass(const Plan& pl, const Workspace& ws, const SortKeys& sk, c
   }
 }
 
+template <class F>
+static void with_sort_threads(int B, bool beside, F&& f) {
+  switch (sort_threads(B, beside)) {
+    case 256: f(std::integral_constant<int, 256>{}); break;
+    case 512: f(std::integral_constant<int, 512>{}); break;
+    default: f(std::integral_constant<int, 1024>{}); break;
+  }
+}
+
+// clear: the first histogram also clears the tables that the steps behind the sort add into (lookups have none)
 void launch_sort_pass(const Plan& pl, const Workspace& ws, const SortKeys& sk, const IdSource& src, int B,
                       int pass, bool beside, bool clear, hipStream_t st,
                       int which /*0 = histogram, 1 = scatter, 2 = column scan*/) {
-  switch (sort_threads(B, beside)) {
-    case 256: sort_pass<256>(pl, ws, sk, src, B, pass, beside, clear, st, which); break;
-    case 512: sort_pass<512>(pl, ws, sk, src, B, pass, beside, clear, st, which); break;
-    default: sort_pass<1024>(pl, ws, sk, src, B, pass, beside, clear, st, which); break;
-  }
+  with_sort_threads(B, beside, [&](auto nt) {
+    sort_pass<nt()>(ws, sk, B, pass, beside, st, which, [&](int blocks, uint32_t* kin, int shift, int bits, bool folds) {
+      auto hist = [&](auto from) {
+        k_sort_hist<nt()><<<blocks, nt(), 0, st>>>(from, kin, B, sk.sentinel, shift, bits, folds, ws.cnt,
+                                                   (uint32_t*)ws.g1_first, clear ? 2 * (int)pl.sh.n1 : 0, ws.ctr);
+      };
+      if (sk.low > 0)  // by prefix
+        hist(PrefixSource{src, sk.low, pl.user_n1, pl.sh.n2, pl.sh.n3});
+      else
+        hist(src);
+    });
+  });
+}
+
+// The same for the ids of a plain table (tt_emb_dense.hip); ws holds what a sort needs.
+void launch_table_sort_pass(const Workspace& ws, const SortKeys& sk, const TableSource& src, int B, int pass,
+                            hipStream_t st, int which) {
+  with_sort_threads(B, false, [&](auto nt) {
+    sort_pass<nt()>(ws, sk, B, pass, false, st, which, [&](int blocks, uint32_t* kin, int shift, int bits, bool folds) {
+      k_sort_hist<nt()><<<blocks, nt(), 0, st>>>(src, kin, B, sk.sentinel, shift, bits, folds, ws.cnt, nullptr, 0,
+                                                 ws.ctr);
+    });
+  });
 }
 
 // The segment kernels of a batch of B items: 1024 threads with 1, 2 or 4 slots each.

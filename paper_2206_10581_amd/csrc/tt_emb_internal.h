@@ -87,6 +87,13 @@ struct PrefixSource {
   uint32_t n1, n2, n3;
 };
 
+// Ids of a plain table of `rows` rows, none of which has the sentinel's number; `padding` is an id that counts as
+// none (negative: there is no such id).
+struct TableSource {
+  const int64_t* ids;
+  int64_t rows, padding;
+};
+
 // What a sort orders by: `bits` bits of the key above the lowest `low`, `per` of them a pass.
 // Out-of-range ids have the key `sentinel`, above every other.  The first pass reads key buffer 1 (which
 // its histogram fills from the ids) and writes the other, the next one back, and so on.
@@ -287,6 +294,32 @@ __host__ __device__ inline int wide_group(int nchunk2, int r) {
   return g;
 }
 
+// Workspace of a plain table's gradient (tt_emb_dense.hip): what a sort of the ids needs, and partial sums of the
+// ids that many positions hold, one row of `stride` floats per tile of sorted slots.
+struct DenseWork {
+  Workspace sort;  // ctr, key, val, cnt, tot
+  float *head, *tail;
+  int stride;
+};
+constexpr int kDenseTile = 32;  // sorted slots of a tile
+
+// Tensors of one launch of the norm and clipping kernels (tt_emb_clip.hip), passed by value: what a launch's
+// arguments hold.  A tensor is cut into units of clip_units(); `first` is its first one in the launch.
+struct ClipItem {
+  const void* in;
+  void* out;
+  int64_t count, first;
+  int32_t type, out_type;
+};
+constexpr int kClipItems = 96;
+constexpr int kClipBlocks = 2048;  // most blocks of such a launch, each of which leaves one partial sum
+struct ClipList {
+  int64_t units;
+  int n;
+  ClipItem item[kClipItems];
+};
+static_assert(sizeof(ClipList) <= 4000, "launch arguments hold 4 KB");
+
 enum KernelSlot {
   kSlotSortHist = 0,
   kSlotSortScan,
@@ -338,6 +371,11 @@ __device__ __forceinline__ uint32_t key_of_id(const PrefixSource& src, int idx, 
   if ((int64_t)row >= src.ids.rows) return sentinel;
   const uint32_t p = row / src.n3, i3 = row - p * src.n3, i1 = p / src.n2, i2 = p - i1 * src.n2;
   return ((i2 * src.n1 + i1) << src.i3_bits) | i3;
+}
+
+__device__ __forceinline__ uint32_t key_of_id(const TableSource& src, int idx, uint32_t sentinel) {
+  const int64_t id = src.ids[idx];
+  return (uint64_t)id >= (uint64_t)src.rows || id == src.padding ? sentinel : (uint32_t)id;
 }
 
 // One entry of a core under the update rule: the SGD step, the Adagrad step  S += dG^2,
