@@ -1000,9 +1000,9 @@ static size_t carve_dense(int cols, int64_t max_batch, char* base, DenseWork* ws
   const int stride = (cols + 3) & ~3;
   DenseWork w{};
   w.sort.ctr = (Counters*)take(sizeof(Counters));
-  for (int k = 0; k < 2; ++k) {
-    w.sort.key[k] = (uint32_t*)take(mB * 4);
-    w.sort.val[k] = (uint32_t*)take(mB * 4);
+  for (int k = 0; k < 2; ++k) {  // the sums read up to kDenseAhead entries behind the last
+    w.sort.key[k] = (uint32_t*)take((mB + kDenseAhead) * 4);
+    w.sort.val[k] = (uint32_t*)take((mB + kDenseAhead) * 4);
   }
   w.sort.cnt = (uint32_t*)take((size_t)sort_blocks_most(max_batch) * kMaxBins * 4);
   w.sort.tot = (uint32_t*)take(kMaxBins * 4);

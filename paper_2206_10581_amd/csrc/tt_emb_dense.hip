@@ -21,14 +21,18 @@ struct Piece<T, 1> {
 };
 
 template <int VEC, class T>
-__device__ __forceinline__ void load_piece(const T* p, float (&x)[VEC]) {
-  const typename Piece<T, VEC>::V v = *(const typename Piece<T, VEC>::V*)p;
+__device__ __forceinline__ void values_of(const typename Piece<T, VEC>::V& v, float (&x)[VEC]) {
   if constexpr (VEC == 1) {
     x[0] = (float)v;
   } else {
 #pragma unroll
     for (int i = 0; i < VEC; ++i) x[i] = (float)v[i];
   }
+}
+
+template <int VEC, class T>
+__device__ __forceinline__ void load_piece(const T* p, float (&x)[VEC]) {
+  values_of<VEC, T>(*(const typename Piece<T, VEC>::V*)p, x);
 }
 
 template <int VEC, class T>
@@ -99,32 +103,31 @@ struct TileRuns {
   bool began;        // the first slot's run began in an earlier tile
   bool head;         // and is a long one: the tile leaves its part
   bool tail;         // the last run begins here and is a long one
-  __device__ __forceinline__ TileRuns(const uint32_t* __restrict__ key, int t, int B, uint32_t none) {
-    s0 = t * kDenseTile;
-    s1 = min(s0 + kDenseTile, B);
+  __device__ __forceinline__ TileRuns(const uint32_t* __restrict__ key, int t, int tile, int B, uint32_t none) {
+    s0 = t * tile;
+    s1 = min(s0 + tile, B);
     first = key[s0];
     last = key[s1 - 1];
-    const bool more = s1 < B;
-    const uint32_t next = more ? key[s1] : none;
-    const uint32_t after = more && s1 + kDenseTile < B ? key[s1 + kDenseTile] : none;
-    began = s0 > 0 && key[max(s0 - 1, 0)] == first;
-    head = began && first < none &&
-           ((t >= 2 && key[max(s0 - kDenseTile - 1, 0)] == first) || next == first);
-    const bool goes_on = last < none && next == last && !(began && first == last);
-    tail = goes_on && after == last;
-    limit = goes_on && !tail ? min(s1 + kDenseTile, B) : s1;
+    const uint32_t prev = key[max(s0 - 1, 0)], prev2 = key[max(s0 - tile - 1, 0)];
+    const uint32_t next = key[min(s1, B - 1)], after = key[min(s1 + tile, B - 1)];
+    began = t >= 1 && prev == first;
+    head = began && first < none && ((t >= 2 && prev2 == first) || (s1 < B && next == first));
+    const bool goes_on = last < none && s1 < B && next == last && !(began && first == last);
+    tail = goes_on && s1 + tile < B && after == last;
+    limit = goes_on && !tail ? min(s1 + tile, B) : s1;
   }
 };
 
 template <class TO, int VEC, bool ADD>
-__device__ __forceinline__ void put_sum(TO* __restrict__ row, int col, int c, float scale, const float (&sum)[VEC]) {
+__device__ __forceinline__ void put_sum(TO* __restrict__ row, int col, int c, float scale, const float (&sum)[VEC],
+                                        const typename Piece<TO, VEC>::V& old) {
   float x[VEC];
   if constexpr (!ADD) {
 #pragma unroll
     for (int i = 0; i < VEC; ++i) x[i] = scale * sum[i];
     store_piece<VEC>(row + col, x);
   } else if (col == c * VEC) {
-    load_piece<VEC>(row + col, x);
+    values_of<VEC, TO>(old, x);
 #pragma unroll
     for (int i = 0; i < VEC; ++i) x[i] = fmaf(scale, sum[i], x[i]);
     store_piece<VEC>(row + col, x);
@@ -138,84 +141,115 @@ __device__ __forceinline__ void put_sum(TO* __restrict__ row, int col, int c, fl
   }
 }
 
-// Sums of the gradient rows of every id whose run of sorted slots a tile owns.
-template <class TI, class TO, int VEC, bool ADD>
+// Sums of the gradient rows of every id whose run of sorted slots a tile owns.  WAVE: a wavefront takes (a part of) one
+// tile, so that keys and positions are scalars and their branches are its own; else 2^lanes threads do.
+// Eight slots at a time: their keys and positions, then all rows (slots that are not the tile's read a row again that
+// it reads anyway), and with ADD the table rows of those that end a run, then the sums in order.
+template <class TI, class TO, int VEC, bool ADD, bool WAVE>
 __global__ __launch_bounds__(kDenseThreads) void k_dense_sum(const uint32_t* __restrict__ key,
-                                                             const uint32_t* __restrict__ pos, int B, uint32_t none,
-                                                             const TI* __restrict__ grad, int64_t ld_grad, int cols,
-                                                             Lanes ln, float scale, TO* __restrict__ out, int64_t ld,
+                                                             const uint32_t* __restrict__ pos, int B, int tile,
+                                                             uint32_t none, const TI* __restrict__ grad,
+                                                             int64_t ld_grad, int cols, Lanes ln, float scale,
+                                                             TO* __restrict__ out, int64_t ld,
                                                              float* __restrict__ head, float* __restrict__ tail,
                                                              int stride) {
-  constexpr int kAhead = 8;
+  typedef typename Piece<TI, VEC>::V VI;
+  typedef typename Piece<TO, VEC>::V VO;
+  constexpr int kAhead = kDenseAhead;
   const int c = (blockIdx.y << ln.lanes) + (threadIdx.x & ((1 << ln.lanes) - 1));
   if (c >= ln.pieces) return;
   const int col = piece_start<VEC>(c, cols), step = gridDim.x * (kDenseThreads >> ln.lanes);
-  const int tiles = (B + kDenseTile - 1) / kDenseTile;
-  for (int t = blockIdx.x * (kDenseThreads >> ln.lanes) + (threadIdx.x >> ln.lanes); t < tiles; t += step) {
-    const TileRuns r(key, t, B, none);
+  const int tiles = (B + tile - 1) / tile;
+  int t = blockIdx.x * (kDenseThreads >> ln.lanes) + (threadIdx.x >> ln.lanes);
+  if constexpr (WAVE) t = __builtin_amdgcn_readfirstlane(t);
+  for (; t < tiles; t += step) {
+    const TileRuns r(key, t, tile, B, none);
     if (r.first >= none) return;  // positions without an id are last
-    uint32_t cur = none;
-    float acc[VEC];
-    auto flush = [&](bool at_end) {
-      if (cur >= none) return;
-      if (r.began && cur == r.first) {
-        store_piece<VEC>(head + (size_t)t * stride + col, acc);
-      } else if (at_end && r.tail) {
-        store_piece<VEC>(tail + (size_t)t * stride + col, acc);
-      } else {
-        put_sum<TO, VEC, ADD>(out + (int64_t)cur * ld, col, c, scale, acc);
-      }
-    };
+    const uint32_t any = pos[r.s0];
+    float acc[VEC] = {};
     for (int s = r.s0; s < r.limit; s += kAhead) {
-      uint32_t k[kAhead];
-      float x[kAhead][VEC];
+      uint32_t k[kAhead + 1], p[kAhead];
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        const int at = min(s + i, B - 1);
-        k[i] = key[at];
-        const bool mine = s + i < r.limit && (s + i < r.s1 || k[i] == r.last) && !(r.began && !r.head && k[i] == r.first);
-        k[i] = mine ? k[i] : none;
-        if (k[i] < none) load_piece<VEC>(grad + pos[at] * ld_grad + col, x[i]);
+      for (int i = 0; i <= kAhead; ++i) k[i] = key[s + i];  // there are some entries behind the last
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) p[i] = pos[s + i];
+      bool mine[kAhead + 1], ends[kAhead];
+#pragma unroll
+      for (int i = 0; i <= kAhead; ++i)
+        mine[i] = s + i < r.limit && k[i] < none && (s + i < r.s1 || k[i] == r.last) &&
+                  !(r.began && !r.head && k[i] == r.first);
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) ends[i] = mine[i] && !(mine[i + 1] && k[i + 1] == k[i]);
+      VI x[kAhead];
+      VO old[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i)
+        x[i] = *(const VI*)(grad + (int64_t)(mine[i] ? p[i] : any) * ld_grad + col);
+      if constexpr (ADD) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+          if (ends[i]) old[i] = *(const VO*)(out + (int64_t)k[i] * ld + col);
       }
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) {
-        if (k[i] >= none) continue;
-        if (k[i] != cur) {
-          flush(false);
-          cur = k[i];
+        if (!mine[i]) continue;
+        float v[VEC];
+        values_of<VEC, TI>(x[i], v);
 #pragma unroll
-          for (int j = 0; j < VEC; ++j) acc[j] = 0.f;
-        }
+        for (int j = 0; j < VEC; ++j) acc[j] += v[j];
+        if (!ends[i]) continue;
+        if (r.began && k[i] == r.first) store_piece<VEC>(head + (size_t)t * stride + col, acc);
+        else if (r.tail && k[i] == r.last) store_piece<VEC>(tail + (size_t)t * stride + col, acc);
+        else put_sum<TO, VEC, ADD>(out + (int64_t)k[i] * ld, col, c, scale, acc, old[i]);
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) acc[j] += x[i][j];
+        for (int j = 0; j < VEC; ++j) acc[j] = 0.f;
       }
     }
-    flush(true);
   }
 }
 
-// Long runs: the parts that their tiles left, in order.
+// Long runs: the parts that their tiles left.  A block looks at kJoinTiles tiles and takes 256 columns; its wavefronts
+// take the parts of a run in turn, and their sums are added in order.
+constexpr int kJoinTiles = 8, kJoinWaves = kDenseThreads / kWave, kJoinCols = kWave * 4;
 template <class TO, bool ADD>
-__global__ __launch_bounds__(kDenseThreads) void k_dense_join(const uint32_t* __restrict__ key, int B, uint32_t none,
-                                                              int cols, float scale, TO* __restrict__ out, int64_t ld,
+__global__ __launch_bounds__(kDenseThreads) void k_dense_join(const uint32_t* __restrict__ key, int B, int tile,
+                                                              uint32_t none, int cols, float scale,
+                                                              TO* __restrict__ out, int64_t ld,
                                                               const float* __restrict__ head,
                                                               const float* __restrict__ tail, int stride) {
-  const int tiles = (B + kDenseTile - 1) / kDenseTile;
-  const int col = blockIdx.y * kDenseThreads + threadIdx.x;
-  for (int t = blockIdx.x; t < tiles; t += gridDim.x) {
-    const TileRuns r(key, t, B, none);
-    if (r.first >= none) return;
-    if (!r.tail || col >= cols) continue;
-    int lo = t + 2, hi = tiles;  // the run covers the first slots of tiles t+1 .. lo-1 at least, never that of hi
-    while (lo < hi) {
-      const int mid = (lo + hi) / 2;
-      if (key[mid * kDenseTile] == r.last) lo = mid + 1;
-      else hi = mid;
-    }
-    float sum[1] = {tail[(size_t)t * stride + col]};
+  __shared__ f4 part[kJoinWaves][kWave];
+  const int tiles = (B + tile - 1) / tile, lane = threadIdx.x % kWave, w = threadIdx.x / kWave;
+  const int col = blockIdx.y * kJoinCols + lane * 4;
+  for (int t0 = blockIdx.x * kJoinTiles; t0 < tiles; t0 += gridDim.x * kJoinTiles) {
+    bool start = false;
+    if (lane < kJoinTiles && t0 + lane < tiles) start = TileRuns(key, t0 + lane, tile, B, none).tail;
+    unsigned long long starts = __ballot(start);  // the same in every wavefront
+    for (; starts != 0; starts &= starts - 1) {
+      const int t = t0 + __ffsll((long long)starts) - 1;
+      const uint32_t id = key[(t + 1) * tile - 1];
+      int lo = t + 3, hi = tiles;  // the run holds the first slots of tiles t+1 .. lo-1 at least, never that of hi
+      while (lo < hi) {
+        const int mid = lo + (hi - lo) / 2;
+        if (key[mid * tile] == id) lo = mid + 1;
+        else hi = mid;
+      }
+      f4 sum = {0.f, 0.f, 0.f, 0.f};
+      if (col < cols) {
+        if (w == 0) sum = *(const f4*)(tail + (size_t)t * stride + col);
 #pragma unroll 8
-    for (int j = t + 1; j < lo; ++j) sum[0] += head[(size_t)j * stride + col];
-    put_sum<TO, 1, ADD>(out + (int64_t)r.last * ld, col, col, scale, sum);
+        for (int j = t + 1 + w; j < lo; j += kJoinWaves) sum += *(const f4*)(head + (size_t)j * stride + col);
+      }
+      part[w][lane] = sum;
+      __syncthreads();
+      if (w == 0 && col < cols) {
+        for (int k = 1; k < kJoinWaves; ++k) sum += part[k][lane];
+        TO* row = out + (int64_t)id * ld + col;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (col + i < cols) row[i] = (TO)(ADD ? fmaf(scale, sum[i], (float)row[i]) : scale * sum[i]);
+      }
+      __syncthreads();
+    }
   }
 }
 
@@ -237,6 +271,17 @@ static void with_piece(int cols, F&& f) {
   constexpr int kVec = 16 / (int)sizeof(T);
   if (cols >= kVec) f(std::integral_constant<int, kVec>{});
   else f(std::integral_constant<int, 1>{});
+}
+
+// The same where a wavefront takes a row: the fewest values a thread that let it hold the row, and 16 bytes where none
+// does.  Narrower pieces keep all lanes at work and fewer sums in registers.
+template <class T, class F>
+static void with_wave_piece(int cols, F&& f) {
+  constexpr int kVec = 16 / (int)sizeof(T);
+  if (cols <= kWave) f(std::integral_constant<int, 1>{});
+  else if (cols <= 2 * kWave) f(std::integral_constant<int, 2>{});
+  else if (kVec == 4 || cols <= 4 * kWave) f(std::integral_constant<int, 4>{});
+  else f(std::integral_constant<int, kVec>{});
 }
 
 static Lanes lanes_of(int cols, int vec) {
@@ -281,21 +326,25 @@ void launch_dense_zero(const tt_emb_matrix& out, hipStream_t st) {
 void launch_dense_sum(const DenseWork& ws, int sorted, int B, const tt_emb_matrix& grad, float scale,
                       const tt_emb_matrix& out, bool add, hipStream_t st) {
   const uint32_t none = (uint32_t)out.rows;
-  const int64_t tiles = (B + kDenseTile - 1) / kDenseTile;
+  const int tile = kDenseTile;
+  const int64_t tiles = (B + tile - 1) / tile;
   with_type(grad.type, [&](auto ti) {
     with_type(out.type, [&](auto to) {
       using TI = decltype(ti);
       using TO = decltype(to);
-      with_piece<TI>(grad.cols, [&](auto vec) {
-        const Lanes ln = lanes_of(grad.cols, vec());
-        auto launch = [&](auto kernel) {
-          kernel<<<grid_of(tiles, ln), kDenseThreads, 0, st>>>(ws.sort.key[sorted], ws.sort.val[sorted], B, none,
-                                                               (const TI*)grad.data, grad.ld, grad.cols, ln, scale,
-                                                               (TO*)out.data, out.ld, ws.head, ws.tail, ws.stride);
-        };
-        if (add) launch(k_dense_sum<TI, TO, vec(), true>);
-        else launch(k_dense_sum<TI, TO, vec(), false>);
-      });
+      auto launch = [&](auto kernel, const Lanes& ln) {
+        kernel<<<grid_of(tiles, ln), kDenseThreads, 0, st>>>(ws.sort.key[sorted], ws.sort.val[sorted], B, tile, none,
+                                                             (const TI*)grad.data, grad.ld, grad.cols, ln, scale,
+                                                             (TO*)out.data, out.ld, ws.head, ws.tail, ws.stride);
+      };
+      auto sums = [&](auto vec, auto wave) {
+        Lanes ln = lanes_of(grad.cols, vec());
+        if (wave()) ln.lanes = std::max(ln.lanes, 6);
+        if (add) launch(k_dense_sum<TI, TO, vec(), true, wave()>, ln);
+        else launch(k_dense_sum<TI, TO, vec(), false, wave()>, ln);
+      };
+      if (grad.cols >= kWave) with_wave_piece<TI>(grad.cols, [&](auto vec) { sums(vec, std::true_type{}); });
+      else with_piece<TI>(grad.cols, [&](auto vec) { sums(vec, std::false_type{}); });
     });
   });
 }
@@ -303,12 +352,13 @@ void launch_dense_sum(const DenseWork& ws, int sorted, int B, const tt_emb_matri
 void launch_dense_join(const DenseWork& ws, int sorted, int B, float scale, const tt_emb_matrix& out, bool add,
                        hipStream_t st) {
   const uint32_t none = (uint32_t)out.rows;
-  const int tiles = (B + kDenseTile - 1) / kDenseTile;
+  const int tile = kDenseTile, tiles = (B + tile - 1) / tile;
   with_type(out.type, [&](auto to) {
     using TO = decltype(to);
-    const dim3 grid((unsigned)std::min(tiles, 1 << 14), (unsigned)(out.cols + kDenseThreads - 1) / kDenseThreads);
+    const dim3 grid((unsigned)std::min((tiles + kJoinTiles - 1) / kJoinTiles, 1 << 14),
+                    (unsigned)(out.cols + kJoinCols - 1) / kJoinCols);
     auto launch = [&](auto kernel) {
-      kernel<<<grid, kDenseThreads, 0, st>>>(ws.sort.key[sorted], B, none, out.cols, scale, (TO*)out.data, out.ld,
+      kernel<<<grid, kDenseThreads, 0, st>>>(ws.sort.key[sorted], B, tile, none, out.cols, scale, (TO*)out.data, out.ld,
                                              ws.head, ws.tail, ws.stride);
     };
     if (add) launch(k_dense_join<TO, true>);

@@ -302,6 +302,7 @@ struct DenseWork {
   int stride;
 };
 constexpr int kDenseTile = 32;  // sorted slots of a tile
+constexpr int kDenseAhead = 8;  // slots whose rows are under way at once
 
 // Tensors of one launch of the norm and clipping kernels (tt_emb_clip.hip), passed by value: what a launch's
 // arguments hold.  A tensor is cut into units of clip_units(); `first` is its first one in the launch.
