@@ -75,14 +75,14 @@ bool table_streamed(const Plan&, int64_t count);
 void launch_table(const Plan&, const float* g1, const float* g2, const float* g3, int64_t first,
                   int64_t count, float* out, hipStream_t);
 // plain tables (tt_emb_dense.hip)
-void launch_table_sort_pass(const Workspace&, const SortKeys&, const TableSource&, int B, int pass, hipStream_t,
-                            int which);
+int launch_table_sort(const Workspace&, const SortKeys&, const TableSource&, int B, const FillJob&, hipStream_t);
 void launch_dense_rows(const tt_emb_matrix& table, const int64_t* ids, int B, float scale, const tt_emb_matrix& out,
                        hipStream_t);
-void launch_dense_zero(const tt_emb_matrix& out, hipStream_t);
+void launch_fill(const FillJob&, hipStream_t);
 void launch_dense_sum(const DenseWork&, int sorted, int B, const tt_emb_matrix& grad, float scale,
                       const tt_emb_matrix& out, bool add, hipStream_t);
-void launch_dense_join(const DenseWork&, int sorted, int B, float scale, const tt_emb_matrix& out, bool add,
+int dense_tile(int B, int cols, int type);
+void launch_dense_join(const DenseWork&, int sorted, int B, int tile, float scale, const tt_emb_matrix& out, bool add,
                        hipStream_t);
 // norm and clipping of many tensors (tt_emb_clip.hip)
 int64_t clip_units(int64_t count);
@@ -996,7 +996,7 @@ static size_t carve_dense(int cols, int64_t max_batch, char* base, DenseWork* ws
     off += (bytes + 255) & ~(size_t)255;
     return p;
   };
-  const size_t mB = (size_t)max_batch, tiles = (mB + kDenseTile - 1) / kDenseTile;
+  const size_t mB = (size_t)max_batch, tiles = (mB + kDenseTileLeast - 1) / kDenseTileLeast;
   const int stride = (cols + 3) & ~3;
   DenseWork w{};
   w.sort.ctr = (Counters*)take(sizeof(Counters));
@@ -1009,6 +1009,7 @@ static size_t carve_dense(int cols, int64_t max_batch, char* base, DenseWork* ws
   w.head = (float*)take(tiles * stride * 4);
   w.tail = (float*)take(tiles * stride * 4);
   w.stride = stride;
+  w.starts = (uint32_t*)take(tiles * 4);
   if (ws != nullptr) *ws = w;
   return off;
 }
@@ -1261,20 +1262,20 @@ int tt_emb_dense_backward(const int64_t* ids, const tt_emb_matrix* grad, float s
     if (workspace_bytes < carve_dense(grad->cols, B, nullptr, nullptr)) return TT_EMB_ENOSPC;
   }
   if (dtable->rows == 0) return TT_EMB_OK;
-  if (!add) launch_dense_zero(*dtable, st);
-  if (B > 0) {
+  const size_t es = type_bytes(dtable->type);
+  FillJob job{(char*)dtable->data, dtable->rows, dtable->ld * (int64_t)es, add ? 0 : dtable->cols * (int)es};
+  if (B == 0) {
+    if (!add) launch_fill(job, st);
+  } else {
     DenseWork ws;
     carve_dense(grad->cols, B, (char*)workspace, &ws);
     const SortKeys sk = sort_keys((uint32_t)dtable->rows, 0);
     const TableSource src{ids, dtable->rows, padding_id};
-    for (int pass = 0; pass < sk.passes; ++pass) {
-      launch_table_sort_pass(ws.sort, sk, src, B, pass, st, 0);
-      if (!sort_folds(sk, B, pass, false)) launch_table_sort_pass(ws.sort, sk, src, B, pass, st, 2);
-      launch_table_sort_pass(ws.sort, sk, src, B, pass, st, 1);
-    }
-    launch_dense_sum(ws, sk.sorted(), B, *grad, scale, *dtable, add != 0, st);
+    const int sorted = launch_table_sort(ws.sort, sk, src, B, job, st);
+    launch_dense_sum(ws, sorted, B, *grad, scale, *dtable, add != 0, st);
     // a run that needs joining covers a whole tile besides those that it starts and ends in
-    if (B > 2 * kDenseTile) launch_dense_join(ws, sk.sorted(), B, scale, *dtable, add != 0, st);
+    const int tile = dense_tile(B, grad->cols, grad->type);
+    if (B > 2 * tile) launch_dense_join(ws, sorted, B, tile, scale, *dtable, add != 0, st);
   }
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? TT_EMB_OK : hip_fail(e);

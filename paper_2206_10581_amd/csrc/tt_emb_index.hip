@@ -301,15 +301,15 @@ struct KeysInPlace {};  // source of the passes behind the first
 // them).  The first pass also clears the tables that later kernels of the same forward add into, and
 // leaves the keys for its scatter, which need not split and renumber the ids again.
 template <int NT, class SRC>
-__global__ __launch_bounds__(NT) void k_sort_hist(
-    SRC src, uint32_t* keys_io, int B, uint32_t N, int shift,
+__device__ __forceinline__ void sort_hist_block(
+    int blk, int nblk, const SRC& src, uint32_t* keys_io, int B, uint32_t N, int shift,
     int bits, bool folds, uint32_t* __restrict__ cnt, uint32_t* zero, int zero_n, Counters* ctr) {
   constexpr bool FROM_IDS = !std::is_same_v<SRC, KeysInPlace>;
   __shared__ uint32_t h[kMaxBins];
   const int tid = threadIdx.x, bins = 1 << bits;
   const uint32_t mask = (uint32_t)bins - 1u;
   const int w = tid / kWave, lane = tid % kWave;
-  const int wbase = blockIdx.x * sort_items(NT) + w * kSortWaveItems;
+  const int wbase = blk * sort_items(NT) + w * kSortWaveItems;
   uint32_t keys[kSteps];
 #pragma unroll
   for (int step = 0; step < kSteps; ++step) {
@@ -325,7 +325,7 @@ __global__ __launch_bounds__(NT) void k_sort_hist(
       const int idx = wbase + step * kWave + lane;
       if (idx < B) keys_io[idx] = keys[step];
     }
-    const int gtid = blockIdx.x * NT + tid, gn = gridDim.x * NT;
+    const int gtid = blk * NT + tid, gn = nblk * NT;
     for (int i = gtid; i < zero_n; i += gn) zero[i] = 0u;
     if (gtid == 0) {
       ctr->err = 0;
@@ -348,11 +348,18 @@ __global__ __launch_bounds__(NT) void k_sort_hist(
   }
   __syncthreads();
   if (folds) {  // a row of 16-bit counts (a block has at most 4096 items)
-    uint32_t* row = cnt + (size_t)blockIdx.x * (padded / 2);
+    uint32_t* row = cnt + (size_t)blk * (padded / 2);
     for (int i = tid; i < padded / 2; i += NT) row[i] = h[2 * i] | (h[2 * i + 1] << 16);
   } else {
-    for (int i = tid; i < bins; i += NT) cnt[(size_t)blockIdx.x * bins + i] = h[i];
+    for (int i = tid; i < bins; i += NT) cnt[(size_t)blk * bins + i] = h[i];
   }
+}
+
+template <int NT, class SRC>
+__global__ __launch_bounds__(NT) void k_sort_hist(
+    SRC src, uint32_t* keys_io, int B, uint32_t N, int shift,
+    int bits, bool folds, uint32_t* __restrict__ cnt, uint32_t* zero, int zero_n, Counters* ctr) {
+  sort_hist_block<NT>((int)blockIdx.x, (int)gridDim.x, src, keys_io, B, N, shift, bits, folds, cnt, zero, zero_n, ctr);
 }
 
 template <int NT, bool FROM_IDS, bool FOLDS>
@@ -370,12 +377,11 @@ __global__ __launch_bounds__(NT) void k_sort_scatter(SortOps<FROM_IDS> ops, int 
 // eight loads in flight per thread, where one thread per column made a chain of them.
 constexpr int kScanThreads = 1024, kScanBins = 32, kScanRuns = kScanThreads / kScanBins;
 constexpr int kScanRows = 8;  // rows of a run that stay in registers
-__global__ __launch_bounds__(kScanThreads) void k_sort_colscan(uint32_t* __restrict__ cnt,
-                                                               uint32_t* __restrict__ tot, int nblk,
-                                                               int bins) {
+__device__ __forceinline__ void sort_colscan_block(int blk, uint32_t* __restrict__ cnt, uint32_t* __restrict__ tot,
+                                                   int nblk, int bins) {
   __shared__ uint32_t part[kScanRuns][kScanBins];
   const int b = threadIdx.x % kScanBins, run = threadIdx.x / kScanBins;
-  const int bin = blockIdx.x * kScanBins + b;
+  const int bin = blk * kScanBins + b;
   const int per = (nblk + kScanRuns - 1) / kScanRuns;
   const int lo = min(run * per, nblk), hi = min(lo + per, nblk);
   uint32_t* col = cnt + min(bin, bins - 1);
@@ -408,6 +414,97 @@ __global__ __launch_bounds__(kScanThreads) void k_sort_colscan(uint32_t* __restr
       if (r0 + k < hi) col[(size_t)(r0 + k) * bins] = before;
       before += c[k];
     }
+  }
+}
+
+__global__ __launch_bounds__(kScanThreads) void k_sort_colscan(uint32_t* __restrict__ cnt, uint32_t* __restrict__ tot,
+                                                               int nblk, int bins) {
+  sort_colscan_block((int)blockIdx.x, cnt, tot, nblk, bins);
+}
+
+// The same three for the ids of a plain table.  The sorts leave most compute units and the memory idle, so blocks
+// behind the first nblk clear the table's gradient meanwhile.
+template <int NT, class SRC>
+__global__ __launch_bounds__(NT) void k_table_hist(SRC src, uint32_t* keys_io, int B, uint32_t N, int shift, int bits,
+                                                   bool folds, uint32_t* __restrict__ cnt, Counters* ctr, int nblk,
+                                                   FillShare fill) {
+  if ((int)blockIdx.x < nblk)
+    sort_hist_block<NT>((int)blockIdx.x, nblk, src, keys_io, B, N, shift, bits, folds, cnt, nullptr, 0, ctr);
+  else
+    fill_share(fill, (int)blockIdx.x - nblk, (int)gridDim.x - nblk);
+}
+
+template <int NT, bool FROM_IDS, bool FOLDS>
+__global__ __launch_bounds__(NT) void k_table_scatter(SortOps<FROM_IDS> ops, int B, int bits,
+                                                      const uint32_t* __restrict__ cnt,
+                                                      const uint32_t* __restrict__ tot, int nblk, FillShare fill) {
+  __shared__ ScatterLds<NT, FOLDS> L;
+  if ((int)blockIdx.x < nblk)
+    stable_scatter_block<NT, FOLDS>(L, (int)blockIdx.x, nblk, B, 1 << bits, cnt, tot, ops);
+  else
+    fill_share(fill, (int)blockIdx.x - nblk, (int)gridDim.x - nblk);
+}
+
+__global__ __launch_bounds__(kScanThreads) void k_table_colscan(uint32_t* __restrict__ cnt, uint32_t* __restrict__ tot,
+                                                                int rows, int bins, int nblk, FillShare fill) {
+  if ((int)blockIdx.x < nblk)
+    sort_colscan_block((int)blockIdx.x, cnt, tot, rows, bins);
+  else
+    fill_share(fill, (int)blockIdx.x - nblk, (int)gridDim.x - nblk);
+}
+
+// Few ids of a plain table are sorted by their ranks alone, in one launch: the rank of a position is the number of
+// smaller keys, and of equal ones in front of it.  A block has G positions, and its threads cut all keys into
+// kRankThreads / G runs; a lane compares its position's key with the keys of one run, four of them a 16-byte word of
+// LDS.  Blocks behind the first nblk clear meanwhile.
+// Keys, and the numbers one above them, are at most 2^31, so the top bit of a difference is the comparison: that takes
+// two and a half instructions, a compare and an add with its carry two and the wait between them.
+constexpr int kRankThreads = 1024;
+constexpr int kRankWords = 2 * kRankMost + 2 * kRankThreads / 8 * 4;  // keys, and the ends of the runs behind them
+__device__ __forceinline__ int less(uint32_t a, uint32_t b) { return (int)((a - b) >> 31); }
+template <int G>
+__global__ __launch_bounds__(kRankThreads) void k_table_rank(TableSource src, int B, uint32_t none, int run,
+                                                             uint32_t* __restrict__ key, uint32_t* __restrict__ pos,
+                                                             int nblk, FillShare fill) {
+  __shared__ __align__(16) uint32_t keys[kRankWords];
+  __shared__ int counts[kRankThreads / kWave][G];
+  if ((int)blockIdx.x >= nblk) {
+    fill_share(fill, (int)blockIdx.x - nblk, (int)gridDim.x - nblk);
+    return;
+  }
+  const int tid = threadIdx.x, lane = tid % kWave, w = tid / kWave, parts = kRankThreads / G;
+  for (int j = tid; j < run * parts; j += kRankThreads) keys[j] = j < B ? key_of_id(src, j, none) : 0x7fffffffu;
+  __syncthreads();
+  const int i0 = (int)blockIdx.x * G, i = i0 + lane % G;
+  const uint32_t mine = keys[min(i, B - 1)];
+  const int j0 = (w * (kWave / G) + lane / G) * run, j1 = j0 + run;
+  const uint4* four = (const uint4*)(keys + j0);
+  int count = 0;
+  if (__ballot(j0 < i0 + G && j1 > i0) == 0) {  // every run lies before the block's positions or behind them
+    const uint32_t below = mine + (j1 <= i0 ? 1u : 0u);
+#pragma unroll 4
+    for (int j = 0; j < run / 4; ++j) {
+      const uint4 k = four[j];
+      count += less(k.x, below) + less(k.y, below) + less(k.z, below) + less(k.w, below);
+    }
+  } else {
+    for (int j = 0; j < run / 4; ++j) {
+      const uint4 k = four[j];
+      const int at = j0 + 4 * j;
+      count += less(k.x, mine + (at < i)) + less(k.y, mine + (at + 1 < i)) + less(k.z, mine + (at + 2 < i)) +
+               less(k.w, mine + (at + 3 < i));
+    }
+  }
+#pragma unroll
+  for (int d = G; d < kWave; d *= 2) count += __shfl_xor(count, d);
+  if (lane < G) counts[w][lane] = count;
+  __syncthreads();
+  if (tid < G && i < B) {
+    int rank = 0;
+#pragma unroll
+    for (int k = 0; k < kRankThreads / kWave; ++k) rank += counts[k][tid];
+    key[rank] = mine;
+    pos[rank] = (uint32_t)i;
   }
 }
 
@@ -776,10 +873,11 @@ __global__ __launch_bounds__(NT) void k_group(
 
 static inline int cdiv(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
-// One of the three kernels of a pass.  first: launches the histogram of the first pass, which reads the ids.
-template <int NT, class FIRST>
-static void sort_pass(const Workspace& ws, const SortKeys& sk, int B, int pass, bool beside, hipStream_t st,
-                      int which, FIRST&& first) {
+// One of the three kernels of a pass.  clear: the first one also clears the tables that the steps
+// behind the sort add into (lookups have none).
+template <int NT>
+static void sort_pass(const Plan& pl, const Workspace& ws, const SortKeys& sk, const IdSource& src, int B,
+                      int pass, bool beside, bool clear, hipStream_t st, int which) {
   const int blocks = cdiv(B, sort_items(NT));
   const int shift = sk.low + pass * sk.per;
   const int bits = sk.bits_of(pass);
@@ -790,11 +888,18 @@ static void sort_pass(const Workspace& ws, const SortKeys& sk, int B, int pass, 
     k_sort_colscan<<<cdiv(1 << bits, kScanBins), kScanThreads, 0, st>>>(ws.cnt, ws.tot, blocks,
                                                                        1 << bits);
   } else if (which == 0) {
+    auto first = [&](auto from) {
+      k_sort_hist<NT><<<blocks, NT, 0, st>>>(
+          from, kin, B, sk.sentinel, shift, bits, folds, ws.cnt, (uint32_t*)ws.g1_first,
+          clear ? 2 * (int)pl.sh.n1 : 0, ws.ctr);
+    };
     if (pass > 0)
       k_sort_hist<NT><<<blocks, NT, 0, st>>>(KeysInPlace{}, kin, B, sk.sentinel, shift, bits, folds, ws.cnt, nullptr, 0,
                                              ws.ctr);
+    else if (sk.low > 0)  // by prefix
+      first(PrefixSource{src, sk.low, pl.user_n1, pl.sh.n2, pl.sh.n3});
     else
-      first(blocks, kin, shift, bits, folds);
+      first(src);
   } else {
     auto scatter = [&](auto kernel, auto ops) { kernel<<<blocks, NT, 0, st>>>(ops, B, bits, ws.cnt, ws.tot); };
     if (pass == 0) {
@@ -807,42 +912,83 @@ static void sort_pass(const Workspace& ws, const SortKeys& sk, int B, int pass, 
   }
 }
 
-template <class F>
-static void with_sort_threads(int B, bool beside, F&& f) {
-  switch (sort_threads(B, beside)) {
-    case 256: f(std::integral_constant<int, 256>{}); break;
-    case 512: f(std::integral_constant<int, 512>{}); break;
-    default: f(std::integral_constant<int, 1024>{}); break;
-  }
-}
-
-// clear: the first histogram also clears the tables that the steps behind the sort add into (lookups have none)
 void launch_sort_pass(const Plan& pl, const Workspace& ws, const SortKeys& sk, const IdSource& src, int B,
                       int pass, bool beside, bool clear, hipStream_t st,
                       int which /*0 = histogram, 1 = scatter, 2 = column scan*/) {
-  with_sort_threads(B, beside, [&](auto nt) {
-    sort_pass<nt()>(ws, sk, B, pass, beside, st, which, [&](int blocks, uint32_t* kin, int shift, int bits, bool folds) {
-      auto hist = [&](auto from) {
-        k_sort_hist<nt()><<<blocks, nt(), 0, st>>>(from, kin, B, sk.sentinel, shift, bits, folds, ws.cnt,
-                                                   (uint32_t*)ws.g1_first, clear ? 2 * (int)pl.sh.n1 : 0, ws.ctr);
-      };
-      if (sk.low > 0)  // by prefix
-        hist(PrefixSource{src, sk.low, pl.user_n1, pl.sh.n2, pl.sh.n3});
-      else
-        hist(src);
-    });
-  });
+  switch (sort_threads(B, beside)) {
+    case 256: sort_pass<256>(pl, ws, sk, src, B, pass, beside, clear, st, which); break;
+    case 512: sort_pass<512>(pl, ws, sk, src, B, pass, beside, clear, st, which); break;
+    default: sort_pass<1024>(pl, ws, sk, src, B, pass, beside, clear, st, which); break;
+  }
 }
 
-// The same for the ids of a plain table (tt_emb_dense.hip); ws holds what a sort needs.
-void launch_table_sort_pass(const Workspace& ws, const SortKeys& sk, const TableSource& src, int B, int pass,
-                            hipStream_t st, int which) {
-  with_sort_threads(B, false, [&](auto nt) {
-    sort_pass<nt()>(ws, sk, B, pass, false, st, which, [&](int blocks, uint32_t* kin, int shift, int bits, bool folds) {
-      k_sort_hist<nt()><<<blocks, nt(), 0, st>>>(src, kin, B, sk.sentinel, shift, bits, folds, ws.cnt, nullptr, 0,
-                                                 ws.ctr);
-    });
-  });
+// Sorts the ids of a plain table into ws.key / ws.val and clears `job` in the same launches; returns which of the two
+// buffers holds them.
+int launch_table_sort(const Workspace& ws, const SortKeys& sk, const TableSource& src, int B, const FillJob& job,
+                      hipStream_t st) {
+  const int clear = job.width != 0 ? kFillBlocks : 0;
+  // Sorting by ranks takes 12 us at 8192 ids and 31 at 16,384, by digits 22 at either; but a large job hides it, and
+  // has to be cut for the launches of the digits (1.05 GB beside 16,384 ids: 177 us in one launch, 216 in four).
+  if (B <= kRankMost || (B <= 2 * kRankMost && job.rows * job.width >= kFillLarge)) {
+    auto rank = [&](auto g) {
+      constexpr int G = g(), parts = kRankThreads / G;
+      // an odd number of 16-byte words: runs side by side in a wavefront start in different banks
+      const int run = 4 * ((((B + parts - 1) / parts + 3) / 4) | 1), nblk = cdiv(B, G);
+      const FillShare all{job, 0, 1, 1};
+      k_table_rank<G><<<nblk + clear, kRankThreads, 0, st>>>(src, B, sk.sentinel, run,
+                                                                                     ws.key[0], ws.val[0], nblk, all);
+    };
+    if (B <= 2048) rank(std::integral_constant<int, 8>{});
+    else if (B <= 4096) rank(std::integral_constant<int, 16>{});
+    else if (B <= 8192) rank(std::integral_constant<int, 32>{});
+    else rank(std::integral_constant<int, 64>{});
+    return 0;
+  }
+  // shares of the job by what the launches take: about twice as long for a scatter as for the others
+  int parts = 0, done = 0;
+  for (int pass = 0; pass < sk.passes; ++pass) parts += sort_folds(sk, B, pass, false) ? 3 : 4;
+  auto share = [&](int n) {
+    done += n;
+    return FillShare{job, done - n, done, parts};
+  };
+  auto sort = [&](auto nt) {
+    constexpr int NT = nt();
+    const int nblk = cdiv(B, sort_items(NT));
+    for (int pass = 0; pass < sk.passes; ++pass) {
+      const int shift = pass * sk.per, bits = sk.bits_of(pass), in = (pass + 1) & 1;
+      const bool folds = sort_folds(sk, B, pass, false);
+      uint32_t *kin = ws.key[in], *vin = ws.val[in], *kout = ws.key[in ^ 1], *vout = ws.val[in ^ 1];
+      auto hist = [&](auto from) {
+        const FillShare f = share(1);
+        k_table_hist<NT><<<nblk + clear, NT, 0, st>>>(from, kin, B, sk.sentinel, shift, bits, folds, ws.cnt,
+                                                                   ws.ctr, nblk, f);
+      };
+      pass == 0 ? hist(src) : hist(KeysInPlace{});
+      if (!folds) {
+        const int cols = cdiv(1 << bits, kScanBins);
+        const FillShare f = share(1);
+        k_table_colscan<<<cols + clear, kScanThreads, 0, st>>>(ws.cnt, ws.tot, nblk, 1 << bits,
+                                                                                     cols, f);
+      }
+      auto scatter = [&](auto kernel, auto ops) {
+        const FillShare f = share(2);
+        kernel<<<nblk + clear, NT, 0, st>>>(ops, B, bits, ws.cnt, ws.tot, nblk, f);
+      };
+      if (pass == 0) {
+        SortOps<true> ops{kin, nullptr, kout, vout, shift, (1u << bits) - 1u};
+        folds ? scatter(k_table_scatter<NT, true, true>, ops) : scatter(k_table_scatter<NT, true, false>, ops);
+      } else {
+        SortOps<false> ops{kin, vin, kout, vout, shift, (1u << bits) - 1u};
+        folds ? scatter(k_table_scatter<NT, false, true>, ops) : scatter(k_table_scatter<NT, false, false>, ops);
+      }
+    }
+  };
+  switch (sort_threads(B, false)) {
+    case 256: sort(std::integral_constant<int, 256>{}); break;
+    case 512: sort(std::integral_constant<int, 512>{}); break;
+    default: sort(std::integral_constant<int, 1024>{}); break;
+  }
+  return sk.sorted();
 }
 
 // The segment kernels of a batch of B items: 1024 threads with 1, 2 or 4 slots each.
