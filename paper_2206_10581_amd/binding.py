@@ -424,14 +424,6 @@ class TTEmbedding:
             pass
 
 
-def _type_of(t):
-    import torch
-    types = {torch.float32: TT_EMB_FP32, torch.bfloat16: TT_EMB_BF16, torch.float16: TT_EMB_FP16}
-    if t.dtype not in types:
-        raise ValueError(f"type {t.dtype}: float32, bfloat16 or float16 needed")
-    return types[t.dtype]
-
-
 class _OnDevice:
     """Device, stream and workspace of the wrappers below."""
 
@@ -439,19 +431,30 @@ class _OnDevice:
         import torch
         if device.type != "cuda":
             raise ValueError(f"tensors on {device}: a GPU needed")
-        self.torch, self.device = torch, device
+        self.torch, self.device, self.index = torch, device, device.index
+        self.lib = load_library()
 
-    def _call(self, name, *args):
-        """The C function `name` with the current stream of this object's device as its last argument."""
-        torch = self.torch
-        stream = torch.cuda.current_stream(self.device).cuda_stream
-        if torch.cuda.current_device() == self.device.index:
-            rc = getattr(_lib, name)(*args, stream)
+    def _call(self, function, *args):
+        """The C function with the current stream of this object's device as its last argument."""
+        cuda = self.torch.cuda
+        if cuda.current_device() == self.index:
+            rc = function(*args, cuda.current_stream(self.index).cuda_stream)
         else:
-            with torch.cuda.device(self.device):
-                rc = getattr(_lib, name)(*args, stream)
+            with cuda.device(self.index):
+                rc = function(*args, cuda.current_stream(self.index).cuda_stream)
         if rc:
-            raise TTEmbError(rc, name)
+            raise TTEmbError(rc, function.__name__)
+
+    def _type(self, t):
+        torch = self.torch
+        kind = t.dtype
+        if kind is torch.float32:
+            return TT_EMB_FP32
+        if kind is torch.bfloat16:
+            return TT_EMB_BF16
+        if kind is torch.float16:
+            return TT_EMB_FP16
+        raise ValueError(f"type {kind}: float32, bfloat16 or float16 needed")
 
     def _make_workspace(self, nbytes):
         self.workspace = self.torch.empty(nbytes + 256, dtype=self.torch.uint8, device=self.device)
@@ -468,7 +471,6 @@ class DenseEmbedding(_OnDevice):
 
     def __init__(self, weight, max_batch: int, scale: float = 1.0, padding_id: int | None = None):
         super().__init__(weight.device)
-        load_library()
         self.weight, self.max_batch, self.scale = weight, int(max_batch), float(scale)
         self.padding_id = -1 if padding_id is None else int(padding_id)
         self._table = self._matrix(weight)
@@ -487,7 +489,7 @@ class DenseEmbedding(_OnDevice):
         step, side = t.stride()
         if cols > 1 and side != 1 or rows > 1 and step < cols:
             raise ValueError(f"strides {t.stride()}: values of a row side by side, rows that do not overlap needed")
-        return TTEmbMatrix(t.data_ptr(), rows, step if rows > 1 else cols, cols, _type_of(t))
+        return TTEmbMatrix(t.data_ptr(), rows, step if rows > 1 else cols, cols, self._type(t))
 
     def _ids(self, ids):
         if ids.dtype != self.torch.int64 or ids.device != self.device or ids.dim() != 1 or not ids.is_contiguous():
@@ -506,9 +508,9 @@ class DenseEmbedding(_OnDevice):
         ptr = self._ids(ids)
         if out is None:
             out = self.torch.empty((ids.numel(), self.dim), dtype=dtype or self.weight.dtype, device=self.device)
-        elif tuple(out.shape) != (ids.numel(), self.dim) or dtype not in (None, out.dtype):
+        elif out.shape != (ids.numel(), self.dim) or dtype not in (None, out.dtype):
             raise ValueError(f"out: {(ids.numel(), self.dim)} of {dtype or out.dtype} needed, not {tuple(out.shape)}")
-        self._call("tt_emb_dense_forward", byref(self._weight()), ptr, self.scale, byref(self._matrix(out)))
+        self._call(self.lib.tt_emb_dense_forward, byref(self._weight()), ptr, self.scale, byref(self._matrix(out)))
         return out
 
     def backward(self, ids, grad_out, out=None, dtype=None, add: bool = False):
@@ -518,7 +520,7 @@ class DenseEmbedding(_OnDevice):
             if add:
                 raise ValueError("add needs out")
             out = self.torch.empty((self.rows, self.dim), dtype=dtype or self.weight.dtype, device=self.device)
-        elif tuple(out.shape) != (self.rows, self.dim) or dtype not in (None, out.dtype):
+        elif out.shape != (self.rows, self.dim) or dtype not in (None, out.dtype):
             raise ValueError(f"out: {(self.rows, self.dim)} of {dtype or out.dtype} needed, not {tuple(out.shape)}")
         self._backward(ids, grad_out, self.scale, self._matrix(out), add)
         return out
@@ -529,9 +531,9 @@ class DenseEmbedding(_OnDevice):
 
     def _backward(self, ids, grad_out, scale, target, add):
         ptr = self._ids(ids)
-        if tuple(grad_out.shape) != (ids.numel(), self.dim):
+        if grad_out.shape != (ids.numel(), self.dim):
             raise ValueError(f"grad_out: {(ids.numel(), self.dim)} needed, not {tuple(grad_out.shape)}")
-        self._call("tt_emb_dense_backward", ptr, byref(self._matrix(grad_out)), scale, self.padding_id, byref(target),
+        self._call(self.lib.tt_emb_dense_backward, ptr, byref(self._matrix(grad_out)), scale, self.padding_id, byref(target),
                    1 if add else 0, self._ws_ptr, self.workspace_bytes)
 
 
@@ -547,7 +549,6 @@ class GradientClip(_OnDevice):
         if not self.tensors:
             raise ValueError("no tensors")
         super().__init__(self.tensors[0].device)
-        load_library()
         self._in = self._values(self.tensors)
         self.out, self._out = None, None
         if out is not None:
@@ -569,7 +570,7 @@ class GradientClip(_OnDevice):
                 raise ValueError(f"tensor on {t.device}, not {self.device}")
             if not (t.is_contiguous() or self._dense(t)):
                 raise ValueError(f"tensor of shape {tuple(t.shape)} and strides {t.stride()} has gaps or overlaps")
-            v.data, v.count, v.type = t.data_ptr(), t.numel(), _type_of(t)
+            v.data, v.count, v.type = t.data_ptr(), t.numel(), self._type(t)
         return values
 
     @staticmethod
@@ -591,13 +592,13 @@ class GradientClip(_OnDevice):
     def norm(self, scale: float = 1.0, out=None):
         """|scale| * the norm, as a float32 on the device."""
         out = self._norm(out)
-        self._call("tt_emb_grad_norm", self._in, len(self._in), float(scale), out.data_ptr(), self._ws_ptr,
+        self._call(self.lib.tt_emb_grad_norm, self._in, len(self._in), float(scale), out.data_ptr(), self._ws_ptr,
                    self.workspace_bytes)
         return out
 
     def clip(self, max_norm: float, scale: float = 1.0, eps: float = 1e-6, out=None):
         """Scales the tensors by scale and down to max_norm; returns the norm before, |scale| included."""
         out = self._norm(out)
-        self._call("tt_emb_grad_clip", self._in, self._out, len(self._in), float(scale), float(max_norm), float(eps),
+        self._call(self.lib.tt_emb_grad_clip, self._in, self._out, len(self._in), float(scale), float(max_norm), float(eps),
                    out.data_ptr(), self._ws_ptr, self.workspace_bytes)
         return out

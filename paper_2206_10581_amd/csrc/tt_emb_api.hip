@@ -86,10 +86,11 @@ void launch_dense_join(const DenseWork&, int sorted, int B, int tile, float scal
                        hipStream_t);
 // norm and clipping of many tensors (tt_emb_clip.hip)
 int64_t clip_units(int64_t count);
-int launch_norm_parts(const ClipList&, double* parts, hipStream_t);
-void launch_norm_total(const double* parts, int n, float scale, float max_norm, float eps, float* norm, double* factor,
-                       hipStream_t);
-void launch_clip(const ClipList&, const double* factor, hipStream_t);
+void launch_put_items(const PutList&, int n, int64_t first, ClipItem* to, hipStream_t);
+int launch_norm_parts(const ClipTensors&, double* parts, hipStream_t);
+void launch_norm_total(const double* parts, int n, float scale, float* norm, hipStream_t);
+void launch_clip(const ClipTensors&, const double* parts, int n, float scale, float max_norm, float eps, float* norm,
+                 hipStream_t);
 hipError_t calibrate(void* buf, size_t bytes, hipStream_t, double* copy_bytes_per_s,
                      double* mfma_flops_per_s, double* gather_bytes_per_s,
                      double* far_gather_bytes_per_s);
@@ -1014,26 +1015,6 @@ static size_t carve_dense(int cols, int64_t max_batch, char* base, DenseWork* ws
   return off;
 }
 
-// Packs the tensors that hold anything into launches' lists, and calls f with each.  out: where they go, or null.
-template <class F>
-static void clip_lists(const tt_emb_values* in, const tt_emb_values* out, int n, F&& f) {
-  ClipList list;
-  list.n = 0;
-  list.units = 0;
-  for (int i = 0; i < n; ++i) {
-    if (in[i].count == 0) continue;
-    const tt_emb_values& to = out != nullptr ? out[i] : in[i];
-    list.item[list.n++] = ClipItem{in[i].data, to.data, in[i].count, list.units, in[i].type, to.type};
-    list.units += clip_units(in[i].count);
-    if (list.n == kClipItems) {
-      f(list);
-      list.n = 0;
-      list.units = 0;
-    }
-  }
-  if (list.n > 0) f(list);
-}
-
 static bool good_values(const tt_emb_values* v, int n) {
   if (n < 0 || (n > 0 && v == nullptr)) return false;
   for (int i = 0; i < n; ++i)
@@ -1043,20 +1024,39 @@ static bool good_values(const tt_emb_values* v, int n) {
   return true;
 }
 
-static size_t norm_bytes(int n) {  // partial sums of every launch, and the factor behind them
-  const int64_t launches = std::max<int64_t>(cdiv64(n, kClipItems), 1);
-  return (size_t)launches * kClipBlocks * sizeof(double) + 256;
-}
+// Workspace: one partial sum a block, and behind them the tensors that do not fit a launch's arguments.
+constexpr size_t kPartsBytes = kClipBlocks * sizeof(double);
+static size_t norm_bytes(int n) { return kPartsBytes + (n > kClipItems ? (size_t)n * sizeof(ClipItem) : 0); }
 
-// Both steps of the norm; factor: also what clipping multiplies with.
-static int run_norm(const tt_emb_values* in, int n, float scale, float max_norm, float eps, float* norm, void* workspace,
-                    double* factor, hipStream_t st) {
-  double* parts = (double*)workspace;
-  int made = 0;
-  clip_lists(in, nullptr, n, [&](const ClipList& list) { made += launch_norm_parts(list, parts + made, st); });
-  launch_norm_total(parts, made, scale, max_norm, eps, norm, factor, st);
-  const hipError_t e = hipGetLastError();
-  return e == hipSuccess ? TT_EMB_OK : hip_fail(e);
+// The tensors that hold anything, as the kernels take them.  out: where they go, or null for in place.
+static ClipTensors clip_tensors(const tt_emb_values* in, const tt_emb_values* out, int n, ClipList* list,
+                                void* workspace, hipStream_t st) {
+  ClipTensors t{list, nullptr, 0, 0, true};
+  for (int i = 0; i < n; ++i) t.n += in[i].count > 0;
+  ClipItem* memory = t.n > kClipItems ? (ClipItem*)((char*)workspace + kPartsBytes) : nullptr;
+  t.many = memory;
+  PutList put;
+  int held = 0;       // tensors in the list that is being filled
+  int64_t first = 0;  // unit of its first one
+  for (int i = 0; i < n; ++i) {
+    if (in[i].count == 0) continue;
+    const tt_emb_values& to = out != nullptr ? out[i] : in[i];
+    t.in_place = t.in_place && to.data == in[i].data && to.type == in[i].type;
+    if (memory == nullptr) {
+      list->item[held++] = ClipItem{in[i].data, to.data, in[i].count, t.units, in[i].type, to.type};
+    } else {
+      if (held == kPutItems) {
+        launch_put_items(put, held, first, memory, st);
+        memory += held;
+        held = 0;
+        first = t.units;
+      }
+      put.item[held++] = PutItem{in[i].data, to.data, in[i].count | (int64_t)(in[i].type | to.type << 2) << kPutTypeBit};
+    }
+    t.units += clip_units(in[i].count);
+  }
+  if (memory != nullptr) launch_put_items(put, held, first, memory, st);
+  return t;
 }
 
 static int check_norm(const tt_emb_values* in, int n, float scale, const float* norm, const void* workspace,
@@ -1291,12 +1291,19 @@ int tt_emb_grad_norm(const tt_emb_values* in, int32_t n, float scale, float* nor
                      size_t workspace_bytes, void* hip_stream) {
   const int rc = check_norm(in, n, scale, norm, workspace, workspace_bytes);
   if (rc != TT_EMB_OK) return rc;
-  return run_norm(in, n, scale, 0.f, 0.f, norm, workspace, nullptr, (hipStream_t)hip_stream);
+  hipStream_t st = (hipStream_t)hip_stream;
+  ClipList list;
+  const ClipTensors t = clip_tensors(in, nullptr, n, &list, workspace, st);
+  double* parts = (double*)workspace;
+  const int made = launch_norm_parts(t, parts, st);
+  launch_norm_total(parts, made, scale, norm, st);
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? TT_EMB_OK : hip_fail(e);
 }
 
 int tt_emb_grad_clip(const tt_emb_values* in, const tt_emb_values* out, int32_t n, float scale, float max_norm,
                      float eps, float* norm, void* workspace, size_t workspace_bytes, void* hip_stream) {
-  int rc = check_norm(in, n, scale, norm, workspace, workspace_bytes);
+  const int rc = check_norm(in, n, scale, norm, workspace, workspace_bytes);
   if (rc != TT_EMB_OK) return rc;
   if (!(max_norm >= 0.f) || !(eps >= 0.f)) return TT_EMB_EINVAL;
   if (out != nullptr) {
@@ -1305,10 +1312,11 @@ int tt_emb_grad_clip(const tt_emb_values* in, const tt_emb_values* out, int32_t 
       if (out[i].count != in[i].count) return TT_EMB_EINVAL;
   }
   hipStream_t st = (hipStream_t)hip_stream;
-  double* factor = (double*)((char*)workspace + norm_bytes(n) - 256);
-  rc = run_norm(in, n, scale, max_norm, eps, norm, workspace, factor, st);
-  if (rc != TT_EMB_OK) return rc;
-  clip_lists(in, out, n, [&](const ClipList& list) { launch_clip(list, factor, st); });
+  ClipList list;
+  const ClipTensors t = clip_tensors(in, out, n, &list, workspace, st);
+  double* parts = (double*)workspace;
+  const int made = launch_norm_parts(t, parts, st);
+  launch_clip(t, parts, made, scale, max_norm, eps, norm, st);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? TT_EMB_OK : hip_fail(e);
 }

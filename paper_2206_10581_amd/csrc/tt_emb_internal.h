@@ -320,8 +320,9 @@ constexpr int64_t kFillLarge = int64_t(1) << 28;
 constexpr int kDenseTileLeast = 8;  // fewest sorted slots of a tile (dense_tile)
 constexpr int kDenseAhead = 8;  // slots whose rows are under way at once
 
-// Tensors of one launch of the norm and clipping kernels (tt_emb_clip.hip), passed by value: what a launch's
-// arguments hold.  A tensor is cut into units of clip_units(); `first` is its first one in the launch.
+// Tensors of the norm and clipping kernels (tt_emb_clip.hip).  A tensor is cut into clip_units() units; `first` is its
+// first one among all.  Up to kClipItems tensors are passed by value, as many as a launch's arguments hold; more are
+// put into memory, kPutItems at a time.
 struct ClipItem {
   const void* in;
   void* out;
@@ -329,13 +330,29 @@ struct ClipItem {
   int32_t type, out_type;
 };
 constexpr int kClipItems = 96;
-constexpr int kClipBlocks = 2048;  // most blocks of such a launch, each of which leaves one partial sum
+// Most blocks of a launch, each of which leaves one partial sum.  With 1024 / 1536 / 2048: norm of 400M values in 300
+// tensors of two types 200 / 191 / 194 us, 300M from bf16 into fp32 541 / 509 / 513, 100M fp32 215 / 219 / 225.
+constexpr int kClipBlocks = 1536;
 struct ClipList {
-  int64_t units;
-  int n;
   ClipItem item[kClipItems];
 };
-static_assert(sizeof(ClipList) <= 4000, "launch arguments hold 4 KB");
+constexpr int kPutItems = 160, kPutTypeBit = 48;  // types above the count, two bits each
+struct PutItem {
+  const void* in;
+  void* out;
+  int64_t count_types;
+};
+struct PutList {
+  PutItem item[kPutItems];
+};
+static_assert(sizeof(ClipList) <= 3900 && sizeof(PutList) <= 3900, "launch arguments hold 4 KB");
+struct ClipTensors {
+  const ClipList* few;
+  const ClipItem* many;  // device, or null
+  int n;
+  int64_t units;
+  bool in_place;  // every tensor goes where it comes from
+};
 
 enum KernelSlot {
   kSlotSortHist = 0,
