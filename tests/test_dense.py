@@ -141,6 +141,38 @@ def test_gradient_long_batches(B, dim, kind):
     _check(got, total, _bound(size, count, 1.0), "float32")
 
 
+@pytest.mark.parametrize("B", [2048, 2049, 4096, 4097, 8192, 8193, 16_384, 16_385])
+@pytest.mark.parametrize("rows,dim", [(5003, 8), (2_900_001, 24)])
+def test_gradient_sorts(rows, dim, B):
+    """Batch sizes at which another sort takes over, beside tables that are cleared quickly and slowly."""
+    import torch
+    import paper_2206_10581_amd as tt
+    ids = _ids(B, rows, B, "hot")
+    grad = _normal(B, (B, dim), "float32")
+    emb = tt.DenseEmbedding(torch.zeros((rows, dim), device="cuda"), B)
+    got = emb.backward(torch.from_numpy(ids).cuda(), grad, out=torch.full((rows, dim), float("nan"), device="cuda"))
+    total, size, count = _sums(ids, grad, rows)
+    _check(got, total, _bound(size, count, 1.0), "float32")
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("rows,dim,gap,lead", [(1, 1, 0, 1), (1, 9, 4, 1), (3, 1, 0, 3), (301, 3, 0, 1), (301, 3, 2, 1),
+                                               (77, 8, 1, 5), (77, 13, 0, 7), (40, 700, 3, 1), (5, 9001, 1, 3)])
+@pytest.mark.parametrize("B", [0, 5])
+def test_gradient_writes_every_row_and_nothing_else(rows, dim, gap, lead, kind, B):
+    import torch
+    import paper_2206_10581_amd as tt
+    flat = torch.full((lead + rows * (dim + gap) + 11,), 7.0, dtype=_torch(kind), device="cuda")
+    out = flat[lead:lead + rows * (dim + gap)].view(rows, dim + gap)[:, :dim]
+    ids = _ids(B, rows, B, "uniform")
+    grad = _normal(dim, (B, dim), "float32")
+    got = tt.DenseEmbedding(out, max(B, 1)).backward(torch.from_numpy(ids).cuda(), grad, out=out)
+    total, size, count = _sums(ids, grad, rows)
+    _check(got, total, _bound(size, count, 1.0), kind)
+    out.fill_(7.0)
+    assert (flat == 7.0).all()
+
+
 def test_gradient_of_padding_and_update():
     import torch
     import paper_2206_10581_amd as tt
