@@ -78,6 +78,9 @@ void launch_table(const Plan&, const float* g1, const float* g2, const float* g3
 int launch_table_sort(const Workspace&, const SortKeys&, const TableSource&, int B, const FillJob&, hipStream_t);
 void launch_dense_rows(const tt_emb_matrix& table, const int64_t* ids, int B, float scale, const tt_emb_matrix& out,
                        hipStream_t);
+bool dense_few(int B, const FillJob&);
+void launch_dense_few(const TableSource&, int B, const tt_emb_matrix& grad, float scale, const tt_emb_matrix& out,
+                      const FillJob&, hipStream_t);
 void launch_fill(const FillJob&, hipStream_t);
 void launch_dense_sum(const DenseWork&, int sorted, int B, const tt_emb_matrix& grad, float scale,
                       const tt_emb_matrix& out, bool add, hipStream_t);
@@ -1266,6 +1269,8 @@ int tt_emb_dense_backward(const int64_t* ids, const tt_emb_matrix* grad, float s
   FillJob job{(char*)dtable->data, dtable->rows, dtable->ld * (int64_t)es, add ? 0 : dtable->cols * (int)es};
   if (B == 0) {
     if (!add) launch_fill(job, st);
+  } else if (dense_few(B, job)) {
+    launch_dense_few(TableSource{ids, dtable->rows, padding_id}, B, *grad, scale, *dtable, job, st);
   } else {
     DenseWork ws;
     carve_dense(grad->cols, B, (char*)workspace, &ws);

@@ -305,6 +305,184 @@ __global__ __launch_bounds__(kJoinThreads) void k_dense_join(const uint32_t* __r
 }
 
 // ---------------------------------------------------------------------------------------------
+// Few positions: one launch, without a sort.  A block has a position and 64 pieces of its row: it looks for the position's
+// id among all of them, leaves if an earlier position has it, and adds up the rows of those that do, eight under way
+// at once, four wavefronts taking eights in turn where there are more than eight.  Blocks in front of these clear the
+// rows whose ids no position has, which they mark in LDS.
+
+constexpr int kFewWaves = kDenseThreads / kWave, kFewLooks = 4;
+
+// Clears the rows of the job that are not marked, as block number b of n (fill_share has the other case).
+__device__ __forceinline__ void fill_unmarked(const FillJob& j, const uint32_t* marks, int b, int n) {
+  const f4 zero = {0.f, 0.f, 0.f, 0.f};
+  const int tid = threadIdx.x, width = j.width;
+  auto marked = [&](int row) { return (marks[row >> 5] >> (row & 31)) & 1u; };
+  if (j.pitch != width && j.rows > 1) {
+    typedef f4 f4_any __attribute__((aligned(2)));
+    const int pieces = (width + 15) / 16;
+    int lanes = 0;
+    while ((1 << lanes) < pieces && (1 << lanes) < kFillThreads) ++lanes;
+    const int per = kFillThreads >> lanes;
+    for (int64_t r = b * per + (tid >> lanes); r < j.rows; r += n * per) {
+      if (marked((int)r)) continue;
+      char* row = j.data + r * j.pitch;
+      for (int c = tid & ((1 << lanes) - 1); c < pieces; c += 1 << lanes) {
+        if (width >= 16) *(f4_any*)(row + min(c * 16, width - 16)) = zero;
+        else
+          for (int i = 0; i < width / 2; ++i) ((uint16_t*)row)[i] = 0;
+      }
+    }
+    return;
+  }
+  // `count` two-byte units from byte `at` on, which lies in `row`, `in` bytes behind its start
+  auto units = [&](int64_t at, int row, int in, int count) {
+    for (int i = 0; i < count; ++i, in += 2) {
+      for (; in >= width; in -= width) ++row;
+      if (!marked(row)) *(uint16_t*)(j.data + at + 2 * i) = 0;
+    }
+  };
+  // Four 16-byte words of a thread at once, 256 words apart: the place in the table of each follows from the one in front
+  // by additions, and their looks at the marks wait together.
+  constexpr int kWords = 4;
+  const int last = (int)j.rows - 1;
+  const int64_t bytes = j.rows * width, lead = min(bytes, (int64_t)(-(uintptr_t)j.data & 15u));
+  const int64_t words = (bytes - lead) / 16, step = (int64_t)n * kWords * kFillThreads;
+  int64_t i = (int64_t)b * kWords * kFillThreads + tid;
+  int row = (int)((lead + i * 16) / width), in = (int)((lead + i * 16) % width);
+  const int step_rows = (int)(step * 16 / width), step_in = (int)(step * 16 % width);
+  const int side_rows = kFillThreads * 16 / width, side_in = kFillThreads * 16 % width;
+  auto move = [&](int& r, int& e, int rows, int bytes_in) {
+    r += rows;
+    e += bytes_in;
+    if (e >= width) {
+      e -= width;
+      ++r;
+    }
+  };
+  for (; i < words; i += step) {
+    int rows[kWords], ins[kWords];
+    uint32_t any[kWords];
+    rows[0] = row;
+    ins[0] = in;
+#pragma unroll
+    for (int k = 1; k < kWords; ++k) {
+      rows[k] = rows[k - 1];
+      ins[k] = ins[k - 1];
+      move(rows[k], ins[k], side_rows, side_in);
+    }
+#pragma unroll
+    for (int k = 0; k < kWords; ++k) {  // words behind the end look at the last row
+      any[k] = marked(min(rows[k], last));
+      int r = rows[k];
+      for (int e = ins[k] + 14; e >= width; e -= width) any[k] |= marked(min(++r, last));
+    }
+#pragma unroll
+    for (int k = 0; k < kWords; ++k) {
+      const int64_t at = i + k * kFillThreads;
+      if (at >= words) break;
+      if (!any[k]) *(f4*)(j.data + lead + at * 16) = zero;
+      else units(lead + at * 16, rows[k], ins[k], 8);
+    }
+    move(row, in, step_rows, step_in);
+  }
+  if (b == 0 && tid == 0) {
+    units(0, 0, 0, (int)(lead / 2));
+    const int64_t at = lead + words * 16;
+    if (at < bytes) units(at, (int)(at / width), (int)(at % width), (int)((bytes - at) / 2));
+  }
+}
+
+template <class TI, class TO, int VEC, bool ADD>
+__global__ __launch_bounds__(kDenseThreads) void k_dense_few(TableSource src, int B, uint32_t none,
+                                                             const TI* __restrict__ grad, int64_t ld_grad, int cols,
+                                                             int pieces, float scale, TO* __restrict__ out, int64_t ld,
+                                                             int clear, FillJob job) {
+  typedef typename Piece<TI, VEC>::V VI;
+  extern __shared__ uint32_t marks[];
+  __shared__ float part[kFewWaves - 1][VEC][kWave];
+  __shared__ uint16_t list[kFewWaves][kFewMost];
+  const int tid = threadIdx.x, lane = tid % kWave, w = tid / kWave;
+  if ((int)blockIdx.x < clear) {
+    for (int i = tid; i < (int)(none + 31) / 32; i += kDenseThreads) marks[i] = 0u;
+    __syncthreads();
+    for (int i = tid; i < B; i += kDenseThreads) {
+      const uint32_t id = key_of_id(src, i, none);
+      if (id < none) atomicOr(&marks[id >> 5], 1u << (id & 31));
+    }
+    __syncthreads();
+    fill_unmarked(job, marks, (int)blockIdx.x, clear);
+    return;
+  }
+  const int slices = (pieces + kWave - 1) / kWave;
+  const int at = (int)blockIdx.x - clear, b = at / slices, c = (at - b * slices) * kWave + lane;
+  const uint32_t id = key_of_id(src, b, none);
+  if (id >= none) return;
+  // the positions that have this id, in order: every wavefront keeps a list of its own
+  int count = 0;
+#pragma unroll 1
+  for (int i0 = 0; i0 < B; i0 += kFewLooks * kWave) {
+    uint32_t k[kFewLooks];
+#pragma unroll
+    for (int m = 0; m < kFewLooks; ++m) k[m] = key_of_id(src, min(i0 + m * kWave + lane, B - 1), none);
+#pragma unroll
+    for (int m = 0; m < kFewLooks; ++m) {
+      const int i = i0 + m * kWave + lane;
+      const bool same = i < B && k[m] == id;
+      const unsigned long long all = __ballot(same);
+      if (same) list[w][count + __popcll(all & ((1ull << lane) - 1ull))] = (uint16_t)i;
+      count += __popcll(all);
+    }
+  }
+  wave_sync();
+  if (list[w][0] != b) return;  // an earlier position has it
+  const int waves = min((count + kDenseAhead - 1) / kDenseAhead, kFewWaves);  // that have rows to add
+  const int col = piece_start<VEC>(min(c, pieces - 1), cols);
+  float acc[VEC] = {};
+  for (int s = w * kDenseAhead; s < count && w < waves; s += 2 * waves * kDenseAhead) {
+    const int s2 = s + waves * kDenseAhead;  // the next eight of this wavefront are asked for with these
+    VI x[2][kDenseAhead];
+    auto ask = [&](VI(&v)[kDenseAhead], int from) {
+#pragma unroll
+      for (int i = 0; i < kDenseAhead; ++i)
+        v[i] = __builtin_nontemporal_load((const VI*)(grad + (int64_t)list[w][min(from + i, count - 1)] * ld_grad + col));
+    };
+    auto add = [&](const VI(&v)[kDenseAhead], int from) {
+      float eight[VEC] = {};  // summed by themselves: no value goes through more than 8 + 16 additions
+#pragma unroll
+      for (int i = 0; i < kDenseAhead; ++i) {
+        if (from + i >= count) continue;
+        float f[VEC];
+        values_of<VEC, TI>(v[i], f);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) eight[j] += f[j];
+      }
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) acc[j] += eight[j];
+    };
+    ask(x[0], s);
+    if (s2 < count) ask(x[1], s2);
+    add(x[0], s);
+    if (s2 < count) add(x[1], s2);
+  }
+  if (waves > 1) {
+    if (w > 0) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) part[w - 1][j][lane] = acc[j];
+    }
+    __syncthreads();
+    if (w == 0)
+      for (int k = 0; k < waves - 1; ++k)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) acc[j] += part[k][j][lane];
+  }
+  if (w != 0 || c >= pieces) return;
+  typename Piece<TO, VEC>::V old{};
+  TO* row = out + (int64_t)id * ld;
+  if constexpr (ADD) old = *(const typename Piece<TO, VEC>::V*)(row + col);
+  put_sum<TO, VEC, ADD>(row, col, c, scale, acc, old);
+}
+
+// ---------------------------------------------------------------------------------------------
 // host-side launchers
 
 template <class F>
@@ -358,6 +536,32 @@ void launch_dense_rows(const tt_emb_matrix& table, const int64_t* ids, int B, fl
         const Lanes ln = lanes_of(table.cols, vec());
         k_dense_rows<TI, TO, vec()><<<grid_of((B + kRowsAhead - 1) / kRowsAhead, ln), kDenseThreads, 0, st>>>(
             (const TI*)table.data, table.ld, table.rows, ids, B, scale, (TO*)out.data, out.ld, table.cols, ln);
+      });
+    });
+  });
+}
+
+bool dense_few(int B, const FillJob& job) {
+  return B <= kFewMost && (job.width == 0 || (job.rows <= kFewRows && job.rows * job.width <= kFewBytes));
+}
+
+void launch_dense_few(const TableSource& src, int B, const tt_emb_matrix& grad, float scale, const tt_emb_matrix& out,
+                      const FillJob& job, hipStream_t st) {
+  const uint32_t none = (uint32_t)out.rows;
+  const bool add = job.width == 0;
+  with_type(grad.type, [&](auto ti) {
+    with_type(out.type, [&](auto to) {
+      using TI = decltype(ti);
+      using TO = decltype(to);
+      with_piece<TI>(grad.cols, [&](auto vec) {
+        const int pieces = (grad.cols + vec() - 1) / vec(), slices = (pieces + kWave - 1) / kWave;
+        const int clear = add ? 0 : kFewClear, lds = add ? 0 : (int)((out.rows + 31) / 32 * 4);
+        auto launch = [&](auto kernel) {
+          kernel<<<clear + B * slices, kDenseThreads, lds, st>>>(src, B, none, (const TI*)grad.data, grad.ld, grad.cols,
+                                                                 pieces, scale, (TO*)out.data, out.ld, clear, job);
+        };
+        if (add) launch(k_dense_few<TI, TO, vec(), true>);
+        else launch(k_dense_few<TI, TO, vec(), false>);
       });
     });
   });

@@ -315,6 +315,13 @@ struct DenseWork {
   int stride;
   uint32_t* starts;  // per tile: the id whose long run starts in it, or none
 };
+// k_dense_few: most ids that are summed in one launch without a sort, beside a table of at most so many rows (a bit of
+// LDS for each) and bytes, and the blocks that clear it.  Against sort, sums and join, us: 129 ids in 32,000 x 512 bf16
+// 8.1 / 15.4, 512 there 10.6 / 17.5 (nine tenths of them the same 22.5 / 17.8), 129 in 32,001 x 2049 28 / 32, 512 in
+// 128,000 x 4096 225 / 176, where the rows' marks cost more than they save.  128 / 256 / 512 blocks: 14.0 / 9.8 / 8.1 at
+// the first.
+constexpr int kFewMost = 512, kFewClear = 512;
+constexpr int64_t kFewRows = 1 << 18, kFewBytes = 1 << 27;
 constexpr int kRankMost = 1 << 13;  // most ids that are sorted by k_table_rank, twice as many beside a large job
 constexpr int64_t kFillLarge = int64_t(1) << 28;
 constexpr int kDenseTileLeast = 8;  // fewest sorted slots of a tile (dense_tile)

@@ -141,6 +141,32 @@ def test_gradient_long_batches(B, dim, kind):
     _check(got, total, _bound(size, count, 1.0), "float32")
 
 
+@pytest.mark.parametrize("B", [1, 2, 8, 9, 33, 64, 65, 500, 512, 513])
+@pytest.mark.parametrize("rows", [1, 7, 31, 32, 33, 1000, 262_144, 262_145])
+@pytest.mark.parametrize("how", ["uniform", "hot", "one", "none"])
+def test_gradient_of_few_positions(rows, B, how):
+    """Rows of three fp16 values: the cleared words hold parts of up to four rows, some of them with positions."""
+    import torch
+    import paper_2206_10581_amd as tt
+    ids = _ids(B + rows, rows, B, how)
+    d_ids = torch.from_numpy(ids).cuda()
+    for dim, kind, lead, gap in ((3, "float16", 1, 0), (1, "bfloat16", 3, 0), (5, "float32", 1, 0), (9, "float16", 0, 4)):
+        if rows > 1000 and gap == 0 and dim != 3:
+            continue
+        flat = torch.full((lead + rows * (dim + gap) + 9,), 7.0, dtype=_torch(kind), device="cuda")
+        out = flat[lead:lead + rows * (dim + gap)].view(rows, dim + gap)[:, :dim]
+        grad = _normal(dim, (B, dim), kind)
+        emb = tt.DenseEmbedding(out, B, scale=0.5)
+        got = emb.backward(d_ids, grad, out=out)
+        total, size, count = _sums(ids, grad, rows)
+        _check(got, 0.5 * total, _bound(size, count, 0.5), kind)
+        base = got.double().cpu().numpy()
+        _check(emb.backward(d_ids, grad, out=out, add=True), base + 0.5 * total,
+               _bound(size, count, 0.5) + 2.0 ** -24 * np.abs(base + 0.5 * total), kind)
+        out.fill_(7.0)
+        assert (flat == 7.0).all()
+
+
 @pytest.mark.parametrize("B", [2048, 2049, 4096, 4097, 8192, 8193, 16_384, 16_385])
 @pytest.mark.parametrize("rows,dim", [(5003, 8), (2_900_001, 24)])
 def test_gradient_sorts(rows, dim, B):
