@@ -90,10 +90,8 @@ void launch_dense_join(const DenseWork&, int sorted, int B, int tile, float scal
 // norm and clipping of many tensors (tt_emb_clip.hip)
 int64_t clip_units(int64_t count);
 void launch_put_items(const PutList&, int n, int64_t first, ClipItem* to, hipStream_t);
-int launch_norm_parts(const ClipTensors&, double* parts, hipStream_t);
-void launch_norm_total(const double* parts, int n, float scale, float* norm, hipStream_t);
-void launch_clip(const ClipTensors&, const double* parts, int n, float scale, float max_norm, float eps, float* norm,
-                 hipStream_t);
+void launch_norm(const ClipTensors&, double* parts, float scale, float* norm, hipStream_t);
+void launch_clip(const ClipTensors&, double* parts, float scale, float max_norm, float eps, float* norm, hipStream_t);
 hipError_t calibrate(void* buf, size_t bytes, hipStream_t, double* copy_bytes_per_s,
                      double* mfma_flops_per_s, double* gather_bytes_per_s,
                      double* far_gather_bytes_per_s);
@@ -1299,9 +1297,7 @@ int tt_emb_grad_norm(const tt_emb_values* in, int32_t n, float scale, float* nor
   hipStream_t st = (hipStream_t)hip_stream;
   ClipList list;
   const ClipTensors t = clip_tensors(in, nullptr, n, &list, workspace, st);
-  double* parts = (double*)workspace;
-  const int made = launch_norm_parts(t, parts, st);
-  launch_norm_total(parts, made, scale, norm, st);
+  launch_norm(t, (double*)workspace, scale, norm, st);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? TT_EMB_OK : hip_fail(e);
 }
@@ -1319,9 +1315,7 @@ int tt_emb_grad_clip(const tt_emb_values* in, const tt_emb_values* out, int32_t 
   hipStream_t st = (hipStream_t)hip_stream;
   ClipList list;
   const ClipTensors t = clip_tensors(in, out, n, &list, workspace, st);
-  double* parts = (double*)workspace;
-  const int made = launch_norm_parts(t, parts, st);
-  launch_clip(t, parts, made, scale, max_norm, eps, norm, st);
+  launch_clip(t, (double*)workspace, scale, max_norm, eps, norm, st);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? TT_EMB_OK : hip_fail(e);
 }

@@ -13,6 +13,10 @@ namespace ttemb {
 
 constexpr int kClipThreads = 256;
 constexpr int kClipUnit = 4096;  // values that a block takes at once
+// Most units that one block does alone, in one launch instead of two.  us a call, and alone, one block / many: norm of
+// 16,000 values in 4 tensors 6.4 / 9.8 and 17.1 / 18.8, of 60,000 in 7 (18 units) 7.8 / 8.6 and 20.5 / 19.2, of 100,000 in
+// 12 (30 units) 11.4 / 9.8; clipping 1000 values 6.6 / 9.0, 16,000 8.4 / 10.7 and 21.3 / 20.6, 60,000 16.1 / 10.7.
+constexpr int kFewNorm = 20, kFewClip = 4;
 
 // P values side by side, aligned like one
 template <class T, int P>
@@ -28,7 +32,7 @@ template <int P, class T, class W, class S>
 __device__ __forceinline__ void unit_values(const T* p, int64_t left, W&& whole, S&& single) {
   typedef typename Some<T, P>::V V;
   constexpr int kStep = kClipThreads * P, kDeep = kClipUnit / kStep;
-  const int at = threadIdx.x * P;
+  const int at = threadIdx.x % kClipThreads * P;
   V v[kDeep];
   if (left >= kClipUnit) {
 #pragma unroll
@@ -101,6 +105,17 @@ __device__ __forceinline__ double block_sum(double v) {
   return s;
 }
 
+// Squares of unit u, which lies in tensor a.
+template <class ITEMS>
+__device__ __forceinline__ double unit_squares(const ITEMS& items, int a, int64_t u) {
+  const int64_t from = (u - items[a].first) * kClipUnit, left = items[a].count - from;
+  const void* in = items[a].in;
+  const int type = items[a].type;
+  if (type == TT_EMB_BF16) return squares((const __bf16*)in + from, left);
+  if (type == TT_EMB_FP16) return squares((const _Float16*)in + from, left);
+  return squares((const float*)in + from, left);
+}
+
 template <class ITEMS>
 __global__ __launch_bounds__(kClipThreads) void k_norm_parts(ITEMS items, int n, int64_t units,
                                                              double* __restrict__ parts) {
@@ -108,12 +123,7 @@ __global__ __launch_bounds__(kClipThreads) void k_norm_parts(ITEMS items, int n,
   int64_t u = blockIdx.x;
   for (int a = item_of(items, n, u); u < units; u += gridDim.x) {
     while (a + 1 < n && items[a + 1].first <= u) ++a;
-    const int64_t from = (u - items[a].first) * kClipUnit, left = items[a].count - from;
-    const void* in = items[a].in;
-    const int type = items[a].type;
-    if (type == TT_EMB_BF16) sum += squares((const __bf16*)in + from, left);
-    else if (type == TT_EMB_FP16) sum += squares((const _Float16*)in + from, left);
-    else sum += squares((const float*)in + from, left);
+    sum += unit_squares(items, a, u);
   }
   sum = block_sum<kClipThreads>(sum);
   if (threadIdx.x == 0) parts[blockIdx.x] = sum;
@@ -159,6 +169,22 @@ __device__ __forceinline__ void scaled_to(const TI* in, void* out, int out_type,
   else scaled(in + from, (float*)out + from, left, f);
 }
 
+template <class ITEMS>
+__device__ __forceinline__ void scale_unit(const ITEMS& items, int a, int64_t u, double f) {
+  const int64_t from = (u - items[a].first) * kClipUnit, left = items[a].count - from;
+  const void* in = items[a].in;
+  void* out = items[a].out;
+  const int type = items[a].type, out_type = items[a].out_type;
+  if (type == TT_EMB_BF16) scaled_to((const __bf16*)in, out, out_type, from, left, f);
+  else if (type == TT_EMB_FP16) scaled_to((const _Float16*)in, out, out_type, from, left, f);
+  else scaled_to((const float*)in, out, out_type, from, left, f);
+}
+
+__device__ __forceinline__ double clip_factor(double norm, float scale, float max_norm, float eps) {
+  const double ratio = (double)max_norm / (norm + (double)eps);
+  return (double)scale * (ratio >= 1.0 ? 1.0 : ratio);  // NaN stays
+}
+
 // Every block adds up the parts of the norm, which costs it less than a launch in between.
 template <class ITEMS>
 __global__ __launch_bounds__(kClipThreads) void k_clip(ITEMS items, int n, int64_t units,
@@ -167,19 +193,34 @@ __global__ __launch_bounds__(kClipThreads) void k_clip(ITEMS items, int n, int64
                                                        float* __restrict__ norm) {
   const double all = total_norm<kClipThreads>(parts, n_parts, scale);
   if (blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)all;
-  const double ratio = (double)max_norm / (all + (double)eps);
-  const double f = (double)scale * (ratio >= 1.0 ? 1.0 : ratio);  // NaN stays
+  const double f = clip_factor(all, scale, max_norm, eps);
   int64_t u = units - 1 - blockIdx.x;
   if (u < 0 || (in_place && f == 1.0)) return;  // nothing changes
   for (int a = item_of(items, n, u); u >= 0; u -= gridDim.x) {
     while (items[a].first > u) --a;
-    const int64_t from = (u - items[a].first) * kClipUnit, left = items[a].count - from;
-    const void* in = items[a].in;
-    void* out = items[a].out;
-    const int type = items[a].type, out_type = items[a].out_type;
-    if (type == TT_EMB_BF16) scaled_to((const __bf16*)in, out, out_type, from, left, f);
-    else if (type == TT_EMB_FP16) scaled_to((const _Float16*)in, out, out_type, from, left, f);
-    else scaled_to((const float*)in, out, out_type, from, left, f);
+    scale_unit(items, a, u, f);
+  }
+}
+
+// Few values: one block does all of it, four units at a time.
+template <bool CLIP>
+__global__ __launch_bounds__(kNormThreads) void k_norm_few(FewItems items, int n, int units, bool in_place, float scale,
+                                                           float max_norm, float eps, float* __restrict__ norm) {
+  const int u0 = threadIdx.x / kClipThreads;
+  double sum = 0.0;
+  for (int u = u0, a = 0; u < units; u += kNormThreads / kClipThreads) {
+    while (a + 1 < n && items[a + 1].first <= u) ++a;
+    sum += unit_squares(items, a, u);
+  }
+  const double all = fabs((double)scale) * sqrt(block_sum<kNormThreads>(sum));
+  if (threadIdx.x == 0) *norm = (float)all;
+  if constexpr (CLIP) {
+    const double f = clip_factor(all, scale, max_norm, eps);
+    if (in_place && f == 1.0) return;  // nothing changes
+    for (int u = u0, a = 0; u < units; u += kNormThreads / kClipThreads) {
+      while (a + 1 < n && items[a + 1].first <= u) ++a;
+      scale_unit(items, a, u, f);
+    }
   }
 }
 
@@ -217,23 +258,31 @@ static void with_items(const ClipTensors& t, F&& f) {
   else f(FewItems{*t.few});
 }
 
-// Returns how many parts it leaves.
-int launch_norm_parts(const ClipTensors& t, double* parts, hipStream_t st) {
+static int launch_norm_parts(const ClipTensors& t, double* parts, hipStream_t st) {  // returns how many it leaves
   const int blocks = (int)std::min<int64_t>(t.units, kClipBlocks);
-  if (blocks > 0)
-    with_items(t, [&](auto items) {
-      k_norm_parts<<<blocks, kClipThreads, 0, st>>>(items, t.n, t.units, parts);
-    });
+  with_items(t, [&](auto items) { k_norm_parts<<<blocks, kClipThreads, 0, st>>>(items, t.n, t.units, parts); });
   return blocks;
 }
-void launch_norm_total(const double* parts, int n, float scale, float* norm, hipStream_t st) {
+
+void launch_norm(const ClipTensors& t, double* parts, float scale, float* norm, hipStream_t st) {
+  if (t.many == nullptr && t.units <= kFewNorm) {
+    k_norm_few<false><<<1, kNormThreads, 0, st>>>(FewItems{*t.few}, t.n, (int)t.units, true, scale, 0.f, 0.f, norm);
+    return;
+  }
+  const int n = launch_norm_parts(t, parts, st);
   k_norm_total<<<1, kNormThreads, 0, st>>>(parts, n, scale, norm);
 }
-void launch_clip(const ClipTensors& t, const double* parts, int n, float scale, float max_norm, float eps, float* norm,
+
+void launch_clip(const ClipTensors& t, double* parts, float scale, float max_norm, float eps, float* norm,
                  hipStream_t st) {
-  const int blocks = (int)std::max<int64_t>(std::min<int64_t>(t.units, kClipBlocks), 1);
+  if (t.many == nullptr && t.units <= kFewClip) {
+    k_norm_few<true><<<1, kNormThreads, 0, st>>>(FewItems{*t.few}, t.n, (int)t.units, t.in_place, scale, max_norm, eps,
+                                                 norm);
+    return;
+  }
+  const int n = launch_norm_parts(t, parts, st);
   with_items(t, [&](auto items) {
-    k_clip<<<blocks, kClipThreads, 0, st>>>(items, t.n, t.units, t.in_place, parts, n, scale, max_norm, eps, norm);
+    k_clip<<<n, kClipThreads, 0, st>>>(items, t.n, t.units, t.in_place, parts, n, scale, max_norm, eps, norm);
   });
 }
 
