@@ -436,15 +436,18 @@ class _OnDevice:
         # the handle alone where torch gives it: making a stream object takes 1 us of a call's 7
         self._stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
             lambda index: torch.cuda.current_stream(index).cuda_stream)
+        self._home = self._stream(self.index)  # the workspace belongs to this stream
 
     def _call(self, function, *args):
         """The C function with the current stream of this object's device as its last argument."""
-        cuda = self.torch.cuda
+        cuda, stream = self.torch.cuda, self._stream(self.index)
+        if stream != self._home:  # its memory is not given to others before this stream is done with it
+            self.workspace.record_stream(cuda.current_stream(self.index))
         if cuda.current_device() == self.index:
-            rc = function(*args, self._stream(self.index))
+            rc = function(*args, stream)
         else:
             with cuda.device(self.index):
-                rc = function(*args, self._stream(self.index))
+                rc = function(*args, stream)
         if rc:
             raise TTEmbError(rc, function.__name__)
 

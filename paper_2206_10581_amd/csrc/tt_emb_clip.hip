@@ -14,9 +14,9 @@ namespace ttemb {
 constexpr int kClipThreads = 256;
 constexpr int kClipUnit = 4096;  // values that a block takes at once
 // Most units that one block does alone, in one launch instead of two.  us a call, and alone, one block / many: norm of
-// 16,000 values in 4 tensors 6.4 / 9.8 and 17.1 / 18.8, of 60,000 in 7 (18 units) 7.8 / 8.6 and 20.5 / 19.2, of 100,000 in
-// 12 (30 units) 11.4 / 9.8; clipping 1000 values 6.6 / 9.0, 16,000 8.4 / 10.7 and 21.3 / 20.6, 60,000 16.1 / 10.7.
-constexpr int kFewNorm = 20, kFewClip = 4;
+// 16,000 values in 4 tensors 6.4 / 10.0 and 16.5 / 18.9, of 60,000 in 7 (18 units) 6.5 / 10.0 and 19.2 / 19.2, of 100,000 in
+// 12 (30 units) 8.9 / 10.1 and 21.4 / 19.0; clipping 1000 values 6.8 / 10.7, 16,000 (7 units) 7.0 / 10.7, 60,000 12.5 / 10.8.
+constexpr int kFewNorm = 24, kFewClip = 10;
 
 // P values side by side, aligned like one
 template <class T, int P>
@@ -206,7 +206,7 @@ __global__ __launch_bounds__(kClipThreads) void k_clip(ITEMS items, int n, int64
 template <bool CLIP>
 __global__ __launch_bounds__(kNormThreads) void k_norm_few(FewItems items, int n, int units, bool in_place, float scale,
                                                            float max_norm, float eps, float* __restrict__ norm) {
-  const int u0 = threadIdx.x / kClipThreads;
+  const int u0 = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kClipThreads);  // a wavefront has one
   double sum = 0.0;
   for (int u = u0, a = 0; u < units; u += kNormThreads / kClipThreads) {
     while (a + 1 < n && items[a + 1].first <= u) ++a;

@@ -337,3 +337,17 @@ def test_refusals():
                 lambda: tt.DenseEmbedding(weight, 0), lambda: tt.DenseEmbedding(weight, 1 << 30)):
         with pytest.raises(tt.TTEmbError):
             bad()
+
+
+def test_a_weight_whose_storage_is_replaced():
+    """The table is looked for where it is at the time of a call."""
+    import torch
+    import paper_2206_10581_amd as tt
+    weight = torch.nn.Parameter(_normal(1, (30, 8), "float32"), requires_grad=False)
+    emb = tt.DenseEmbedding(weight, 4)
+    ids = torch.tensor([3, 29, 0], device="cuda")
+    assert torch.equal(emb.forward(ids), weight[ids])
+    weight.data = _normal(2, (30, 8), "float32")
+    assert torch.equal(emb.forward(ids), weight[ids])
+    weight.data = _normal(3, (30, 8), "bfloat16")
+    assert torch.equal(emb.forward(ids), weight[ids])
