@@ -10,6 +10,9 @@
  *                    the parameter update on the device (paper: Section 5, the "bwd" and "upd"
  *                    phases of the timing breakdown; the paper prints no formula and names no
  *                    optimiser, so this is the chain rule through the two products and plain SGD)
+ * and, for what is trained beside such a table, lookups and gradients of plain tables
+ * (tt_emb_dense_forward, tt_emb_dense_backward) and the norm and clipping of a step's gradients
+ * (tt_emb_grad_norm, tt_emb_grad_clip), which need no handle.
  *
  * Naming.  The table has N = n1*n2*n3 rows (paper: M = m1 m2 m3) of D = d1*d2*d3 floats
  * (paper: N = n1 n2 n3); the TT ranks are (1, r1, r2, 1) (paper: R_0..R_3 with R_0 = R_3 = 1).

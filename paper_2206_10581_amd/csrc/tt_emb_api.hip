@@ -85,6 +85,7 @@ void launch_fill(const FillJob&, hipStream_t);
 void launch_dense_sum(const DenseWork&, int sorted, int B, const tt_emb_matrix& grad, float scale,
                       const tt_emb_matrix& out, bool add, hipStream_t);
 int dense_tile(int B, int cols, int type);
+int64_t dense_tiles_most(int cols, int64_t max_batch);
 void launch_dense_join(const DenseWork&, int sorted, int B, int tile, float scale, const tt_emb_matrix& out, bool add,
                        hipStream_t);
 // norm and clipping of many tensors (tt_emb_clip.hip)
@@ -998,7 +999,7 @@ static size_t carve_dense(int cols, int64_t max_batch, char* base, DenseWork* ws
     off += (bytes + 255) & ~(size_t)255;
     return p;
   };
-  const size_t mB = (size_t)max_batch, tiles = (mB + kDenseTileLeast - 1) / kDenseTileLeast;
+  const size_t mB = (size_t)max_batch, tiles = (size_t)dense_tiles_most(cols, max_batch);
   const int stride = (cols + 3) & ~3;
   DenseWork w{};
   w.sort.ctr = (Counters*)take(sizeof(Counters));

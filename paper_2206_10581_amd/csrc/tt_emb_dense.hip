@@ -576,10 +576,18 @@ void launch_fill(const FillJob& job, hipStream_t st) {
 // 13.9, 5003 of 1001 fp16 7.2 / 10.2 / 17.4, 50,000 of 24 fp32 8.3 / 13.1 / 19.8, 8192 of 2048 bf16 18.4 / 17.2 / 20.5,
 // 16,384 of 4096 bf16 45.8 / 43.1 / 45.4, 200,000 of 128 fp32 33.6 / 35.0 / 39.7.  Sums and joins together with 8 / 16:
 // 20,000 rows of 512 bf16 16.7 / 19.2, 65,536 of 256 23.1 / 21.4, 100,000 of 128 26.0 / 24.2.
+constexpr int64_t kTileFewPieces = (int64_t)64 << 16;
+constexpr int kTileFewIds = 1 << 16;
 int dense_tile(int B, int cols, int type) {
   const int piece = type == TT_EMB_FP32 ? 4 : 8;
-  const bool few = (int64_t)B * ((cols + piece - 1) / piece) <= (int64_t)64 << 16 && B < 1 << 16;
+  const bool few = (int64_t)B * ((cols + piece - 1) / piece) <= kTileFewPieces && B < kTileFewIds;
   return few ? kDenseTileLeast : 2 * kDenseTileLeast;
+}
+// Most tiles of any batch of up to max_batch rows.
+int64_t dense_tiles_most(int cols, int64_t max_batch) {
+  const int64_t few = std::min<int64_t>({max_batch, kTileFewIds - 1, kTileFewPieces / ((cols + 7) / 8)});
+  return std::max((few + kDenseTileLeast - 1) / kDenseTileLeast,
+                  (max_batch + 2 * kDenseTileLeast - 1) / (2 * kDenseTileLeast));
 }
 
 void launch_dense_sum(const DenseWork& ws, int sorted, int B, const tt_emb_matrix& grad, float scale,

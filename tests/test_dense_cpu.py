@@ -48,6 +48,17 @@ def test_dense_workspace():
         assert [n for _, n in sizes[k:k + 8]] == sorted(n for _, n in sizes[k:k + 8])   # a workspace fits all smaller batches
 
 
+@pytest.mark.parametrize("cols", [1, 63, 512, 4096, 65536])
+def test_a_workspace_fits_every_smaller_batch(cols):
+    """Tiles of sorted positions get larger where batches do: the smaller ones must not need more."""
+    pieces = (cols + 7) // 8
+    turn = [min(65535, (64 << 16) // pieces), 65536, (64 << 16) // pieces]
+    batches = sorted({max(1, n + d) for n in (1, 8, 100, *turn) for d in (-1, 0, 1)} | {2 * n for n in turn})
+    need = [b.tt_emb_dense_workspace_bytes(cols, n) for n in batches if n < 1 << 30]
+    assert all(rc == 0 for rc, _ in need)
+    assert [n for _, n in need] == sorted(n for _, n in need)
+
+
 def test_dense_backward_checks():
     good, ws = _m(), b.tt_emb_dense_workspace_bytes(16, 10)[1]
 
