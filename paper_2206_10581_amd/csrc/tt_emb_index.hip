@@ -454,57 +454,61 @@ __global__ __launch_bounds__(kScanThreads) void k_table_colscan(uint32_t* __rest
 }
 
 // Few ids of a plain table are sorted by their ranks alone, in one launch: the rank of a position is the number of
-// smaller keys, and of equal ones in front of it.  A block has G positions, and its threads cut all keys into
-// kRankThreads / G runs; a lane compares its position's key with the keys of one run, four of them a 16-byte word of
-// LDS.  Blocks behind the first nblk clear meanwhile.
-// Keys, and the numbers one above them, are at most 2^31, so the top bit of a difference is the comparison: that takes
-// two and a half instructions, a compare and an add with its carry two and the wait between them.
-constexpr int kRankThreads = 1024;
-constexpr int kRankWords = 2 * kRankMost + 2 * kRankThreads / 8 * 4;  // keys, and the ends of the runs behind them
-__device__ __forceinline__ int less(uint32_t a, uint32_t b) { return (int)((a - b) >> 31); }
+// smaller keys, and of equal ones in front of it.  A block has G positions.  Its wavefronts share all keys, K times 64 of
+// them each, one a lane; a position's key is a scalar that a wavefront compares with its keys, and the lanes that
+// are smaller are counted as one number: an instruction for 64 comparisons and two scalar ones, which bound it.  (With
+// positions in the lanes and keys from LDS 8192 ids took 11.6 us instead of 10.0.)  Blocks behind the first nblk clear
+// meanwhile.
+constexpr int kRankThreads = 1024, kRankWaves = kRankThreads / kWave;
 template <int G>
-__global__ __launch_bounds__(kRankThreads) void k_table_rank(TableSource src, int B, uint32_t none, int run,
+__global__ __launch_bounds__(kRankThreads) void k_table_rank(TableSource src, int B, uint32_t none,
                                                              uint32_t* __restrict__ key, uint32_t* __restrict__ pos,
                                                              int nblk, FillShare fill) {
-  __shared__ __align__(16) uint32_t keys[kRankWords];
-  __shared__ int counts[kRankThreads / kWave][G];
+  constexpr int K = rank_most(G) / kRankThreads;
+  __shared__ int counts[kRankWaves][G];
   if ((int)blockIdx.x >= nblk) {
     fill_share(fill, (int)blockIdx.x - nblk, (int)gridDim.x - nblk);
     return;
   }
-  const int tid = threadIdx.x, lane = tid % kWave, w = tid / kWave, parts = kRankThreads / G;
-  for (int j = tid; j < run * parts; j += kRankThreads) keys[j] = j < B ? key_of_id(src, j, none) : 0x7fffffffu;
-  __syncthreads();
-  const int i0 = (int)blockIdx.x * G, i = i0 + lane % G;
-  const uint32_t mine = keys[min(i, B - 1)];
-  const int j0 = (w * (kWave / G) + lane / G) * run, j1 = j0 + run;
-  const uint4* four = (const uint4*)(keys + j0);
-  int count = 0;
-  if (__ballot(j0 < i0 + G && j1 > i0) == 0) {  // every run lies before the block's positions or behind them
-    const uint32_t below = mine + (j1 <= i0 ? 1u : 0u);
-#pragma unroll 4
-    for (int j = 0; j < run / 4; ++j) {
-      const uint4 k = four[j];
-      count += less(k.x, below) + less(k.y, below) + less(k.z, below) + less(k.w, below);
+  const int tid = threadIdx.x, lane = tid % kWave, w = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int run = (B + kRankThreads - 1) / kRankThreads * kWave;  // keys of a wavefront
+  const int i0 = (int)blockIdx.x * G, j0 = w * run;
+  const uint32_t mine = key_of_id(src, min(i0 + lane, B - 1), none);
+  uint32_t k[K];
+#pragma unroll
+  for (int c = 0; c < K; ++c) k[c] = key_of_id(src, min(j0 + c * kWave + lane, B - 1), none);
+#pragma unroll
+  for (int c = 0; c < K; ++c)
+    if (c * kWave >= run || j0 + c * kWave + lane >= B) k[c] = 0xffffffffu;  // greater than any
+  int count = 0;  // of position i0 + lane
+  if (j0 + run <= i0 || j0 >= i0 + G) {
+    const uint32_t more = j0 < i0 ? 1u : 0u;  // in front of all positions equal keys count as smaller
+#pragma unroll 2
+    for (int i = 0; i < G; ++i) {
+      const uint32_t below = (uint32_t)__builtin_amdgcn_readlane((int)mine, i) + more;
+      int n = 0;
+#pragma unroll
+      for (int c = 0; c < K; ++c) n += __popcll(__ballot(k[c] < below));
+      count = lane == i ? n : count;
     }
   } else {
-    for (int j = 0; j < run / 4; ++j) {
-      const uint4 k = four[j];
-      const int at = j0 + 4 * j;
-      count += less(k.x, mine + (at < i)) + less(k.y, mine + (at + 1 < i)) + less(k.z, mine + (at + 2 < i)) +
-               less(k.w, mine + (at + 3 < i));
+    for (int i = 0; i < G; ++i) {
+      const uint32_t at = (uint32_t)__builtin_amdgcn_readlane((int)mine, i);
+      int n = 0;
+#pragma unroll
+      for (int c = 0; c < K; ++c)
+        n += __popcll(__ballot(k[c] < at + (uint32_t)(j0 + c * kWave + lane < i0 + i)));
+      count = lane == i ? n : count;
     }
   }
-#pragma unroll
-  for (int d = G; d < kWave; d *= 2) count += __shfl_xor(count, d);
   if (lane < G) counts[w][lane] = count;
   __syncthreads();
-  if (tid < G && i < B) {
+  if (tid < G && i0 + tid < B) {
     int rank = 0;
 #pragma unroll
-    for (int k = 0; k < kRankThreads / kWave; ++k) rank += counts[k][tid];
+    for (int v = 0; v < kRankWaves; ++v) rank += counts[v][tid];
     key[rank] = mine;
-    pos[rank] = (uint32_t)i;
+    pos[rank] = (uint32_t)(i0 + tid);
   }
 }
 
@@ -927,20 +931,17 @@ void launch_sort_pass(const Plan& pl, const Workspace& ws, const SortKeys& sk, c
 int launch_table_sort(const Workspace& ws, const SortKeys& sk, const TableSource& src, int B, const FillJob& job,
                       hipStream_t st) {
   const int clear = job.width != 0 ? kFillBlocks : 0;
-  // Sorting by ranks takes 12 us at 8192 ids and 31 at 16,384, by digits 22 at either; but a large job hides it, and
+  // Sorting by ranks takes 10 us at 8192 ids and 32 at 16,384, by digits 22 at either; but a large job hides it, and
   // has to be cut for the launches of the digits (1.05 GB beside 16,384 ids: 177 us in one launch, 216 in four).
   if (B <= kRankMost || (B <= 2 * kRankMost && job.rows * job.width >= kFillLarge)) {
     auto rank = [&](auto g) {
-      constexpr int G = g(), parts = kRankThreads / G;
-      // an odd number of 16-byte words: runs side by side in a wavefront start in different banks
-      const int run = 4 * ((((B + parts - 1) / parts + 3) / 4) | 1), nblk = cdiv(B, G);
-      const FillShare all{job, 0, 1, 1};
-      k_table_rank<G><<<nblk + clear, kRankThreads, 0, st>>>(src, B, sk.sentinel, run,
-                                                                                     ws.key[0], ws.val[0], nblk, all);
+      const int nblk = cdiv(B, g());
+      k_table_rank<g()><<<nblk + clear, kRankThreads, 0, st>>>(src, B, sk.sentinel, ws.key[0], ws.val[0], nblk,
+                                                               FillShare{job, 0, 1, 1});
     };
-    if (B <= 2048) rank(std::integral_constant<int, 8>{});
-    else if (B <= 4096) rank(std::integral_constant<int, 16>{});
-    else if (B <= 8192) rank(std::integral_constant<int, 32>{});
+    if (B <= rank_most(8)) rank(std::integral_constant<int, 8>{});
+    else if (B <= rank_most(16)) rank(std::integral_constant<int, 16>{});
+    else if (B <= rank_most(32)) rank(std::integral_constant<int, 32>{});
     else rank(std::integral_constant<int, 64>{});
     return 0;
   }

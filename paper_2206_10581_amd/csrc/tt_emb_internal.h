@@ -324,6 +324,7 @@ constexpr int kFewMost = 512, kFewClear = 512;
 constexpr int64_t kFewRows = 1 << 18, kFewBytes = 1 << 27;
 constexpr int kRankMost = 1 << 13;  // most ids that are sorted by k_table_rank, twice as many beside a large job
 constexpr int64_t kFillLarge = int64_t(1) << 28;
+__host__ __device__ constexpr int rank_most(int positions) { return 256 * positions; }  // ids, by positions of a block
 constexpr int kDenseTileLeast = 8;  // fewest sorted slots of a tile (dense_tile)
 constexpr int kDenseAhead = 8;  // slots whose rows are under way at once
 
