@@ -63,17 +63,42 @@ struct ManyItems {
   __device__ __forceinline__ const ClipItem& operator[](int a) const { return item[a]; }
 };
 
-// The last tensor that starts at or before unit u.
-template <class ITEMS>
-__device__ __forceinline__ int item_of(const ITEMS& items, int n, int64_t u) {
-  int a = 0, b = n - 1;
-  while (a < b) {
-    const int mid = (a + b + 1) / 2;
+// The last of the tensors lo .. hi-1 that starts at or before unit u, which tensor lo does.
+__device__ __forceinline__ int item_of(const FewItems& items, int lo, int hi, int64_t u) {
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
     const bool before = items[mid].first <= u;
-    a = before ? mid : a;
-    b = before ? b : mid - 1;
+    lo = before ? mid : lo;
+    hi = before ? hi : mid;
   }
-  return a;
+  return lo;
+}
+// In memory: a wavefront looks at 64 places at once.
+__device__ __forceinline__ int item_of(const ManyItems& items, int lo, int hi, int64_t u) {
+  const int lane = threadIdx.x % kWave;
+  while (hi - lo > 1) {
+    const int step = (hi - lo + kWave - 1) / kWave, at = lo + lane * step;
+    const int k = __popcll(__ballot(at < hi && items[min(at, hi - 1)].first <= u)) - 1;
+    lo += k * step;
+    hi = min(hi, lo + step);
+  }
+  return lo;
+}
+
+// From one unit of a block to its next: a few tensors on (or back), or a search over what is left.  300M values in 300
+// tensors 499 to 509 us with 8 to 16 steps, 537 with 3; 11M values in 290 tensors 31 to 36, 87 with steps alone.
+constexpr int kItemSteps = 12;
+template <class ITEMS>
+__device__ __forceinline__ int next_item(const ITEMS& items, int a, int n, int64_t u) {
+  for (int i = 0; i < kItemSteps; ++i, ++a)
+    if (a + 1 >= n || items[a + 1].first > u) return a;
+  return item_of(items, a, n, u);
+}
+template <class ITEMS>
+__device__ __forceinline__ int earlier_item(const ITEMS& items, int a, int64_t u) {
+  for (int i = 0; i < kItemSteps; ++i, --a)
+    if (items[a].first <= u) return a;
+  return item_of(items, 0, a + 1, u);
 }
 
 template <class T>
@@ -121,8 +146,8 @@ __global__ __launch_bounds__(kClipThreads) void k_norm_parts(ITEMS items, int n,
                                                              double* __restrict__ parts) {
   double sum = 0.0;
   int64_t u = blockIdx.x;
-  for (int a = item_of(items, n, u); u < units; u += gridDim.x) {
-    while (a + 1 < n && items[a + 1].first <= u) ++a;
+  for (int a = item_of(items, 0, n, u); u < units; u += gridDim.x) {
+    a = next_item(items, a, n, u);
     sum += unit_squares(items, a, u);
   }
   sum = block_sum<kClipThreads>(sum);
@@ -196,8 +221,8 @@ __global__ __launch_bounds__(kClipThreads) void k_clip(ITEMS items, int n, int64
   const double f = clip_factor(all, scale, max_norm, eps);
   int64_t u = units - 1 - blockIdx.x;
   if (u < 0 || (in_place && f == 1.0)) return;  // nothing changes
-  for (int a = item_of(items, n, u); u >= 0; u -= gridDim.x) {
-    while (items[a].first > u) --a;
+  for (int a = item_of(items, 0, n, u); u >= 0; u -= gridDim.x) {
+    a = earlier_item(items, a, u);
     scale_unit(items, a, u, f);
   }
 }

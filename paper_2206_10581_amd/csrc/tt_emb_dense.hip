@@ -220,12 +220,12 @@ __global__ __launch_bounds__(kDenseThreads) void k_dense_sum(const uint32_t* __r
 }
 
 // Long runs: the parts that their tiles left are added in a fixed order.  A block looks at 64 tiles and takes 128
-// columns; 32 lanes have four columns each, and the halves of a wavefront take a run's parts in turn.  A wavefront
-// takes a run of its own, but all of them the one run of a block that has more than 64 parts.  65,536 ids, half of
+// columns; a lane has four of them, and the halves (of narrower rows smaller parts) of a wavefront take a run's
+// parts in turn.  A wavefront takes a run of its own, but all of them the one run of a block that has more than 64 parts.  65,536 ids, half of
 // them the same, rows of 1024 bf16: 88 us with four wavefronts on every run and its end looked for from 64 tiles to
 // the next 64, 25 so.  64 columns a block take 17 there, but 15 instead of 9 at 16,384 rows of 4096.
 constexpr int kJoinThreads = 1024, kJoinWaves = kJoinThreads / kWave, kJoinTiles = kWave, kJoinCols = 128;
-constexpr int kJoinLanes = kJoinCols / 4, kJoinGroups = kWave / kJoinLanes;
+constexpr int kJoinLanes = kJoinCols / 4;  // at most
 constexpr int kJoinAhead = 8;  // parts under way at once
 template <class TO, bool ADD>
 __global__ __launch_bounds__(kJoinThreads) void k_dense_join(const uint32_t* __restrict__ key, int B, int tile,
@@ -233,10 +233,10 @@ __global__ __launch_bounds__(kJoinThreads) void k_dense_join(const uint32_t* __r
                                                              TO* __restrict__ out, int64_t ld,
                                                              const float* __restrict__ head,
                                                              const float* __restrict__ tail, int stride,
-                                                             const uint32_t* __restrict__ start_ids) {
+                                                             const uint32_t* __restrict__ start_ids, int lanes) {
   __shared__ f4 part[kJoinWaves][kJoinLanes];
   const int tiles = (B + tile - 1) / tile, lane = threadIdx.x % kWave, w = threadIdx.x / kWave;
-  const int col = blockIdx.y * kJoinCols + lane % kJoinLanes * 4, group = lane / kJoinLanes;
+  const int groups = kWave / lanes, group = lane / lanes, col = blockIdx.y * kJoinCols + lane % lanes * 4;
   // parts number p, p + step, ... of the run that starts in tile t, the first in `tail`, added over a wavefront
   auto sum_of = [&](int t, int parts, int p, int step) {
     f4 sum = {0.f, 0.f, 0.f, 0.f};
@@ -251,8 +251,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_dense_join(const uint32_t* __r
       for (int i = 0; i < kJoinAhead; ++i)
         if (p + i * step < parts) sum += v[i];
     }
-#pragma unroll
-    for (int d = kJoinLanes; d < kWave; d *= 2)
+    for (int d = lanes; d < kWave; d *= 2)
 #pragma unroll
       for (int i = 0; i < 4; ++i) sum[i] += __shfl_xor(sum[i], d);
     return sum;
@@ -261,7 +260,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_dense_join(const uint32_t* __r
     TO* row = out + (int64_t)id * ld + col;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      if (lane < kJoinLanes && col + i < cols) row[i] = (TO)(ADD ? fmaf(scale, sum[i], (float)row[i]) : scale * sum[i]);
+      if (lane < lanes && col + i < cols) row[i] = (TO)(ADD ? fmaf(scale, sum[i], (float)row[i]) : scale * sum[i]);
   };
   for (int t0 = blockIdx.x * kJoinTiles; t0 < tiles; t0 += gridDim.x * kJoinTiles) {
     const uint32_t start_id = start_ids[min(t0 + lane, tiles - 1)];
@@ -288,15 +287,15 @@ __global__ __launch_bounds__(kJoinThreads) void k_dense_join(const uint32_t* __r
         step = (hi - end + kWave - 1) / kWave;
       }
       if (end - t <= kWave) {  // every run but the last of the 64 tiles is such a one
-        if (n % kJoinWaves == w) put(id, sum_of(t, end - t, group, kJoinGroups));
+        if (n % kJoinWaves == w) put(id, sum_of(t, end - t, group, groups));
         continue;
       }
-      const f4 sum = sum_of(t, end - t, w * kJoinGroups + group, kJoinWaves * kJoinGroups);
-      if (lane < kJoinLanes) part[w][lane] = sum;
+      const f4 sum = sum_of(t, end - t, w * groups + group, kJoinWaves * groups);
+      if (lane < lanes) part[w][lane] = sum;
       __syncthreads();
       if (w == 0) {
-        f4 all = part[0][lane % kJoinLanes];
-        for (int k = 1; k < kJoinWaves; ++k) all += part[k][lane % kJoinLanes];
+        f4 all = part[0][lane % lanes];
+        for (int k = 1; k < kJoinWaves; ++k) all += part[k][lane % lanes];
         put(id, all);
       }
       __syncthreads();
@@ -310,7 +309,8 @@ __global__ __launch_bounds__(kJoinThreads) void k_dense_join(const uint32_t* __r
 // at once, four wavefronts taking eights in turn where there are more than eight.  Blocks in front of these clear the
 // rows whose ids no position has, which they mark in LDS.
 
-constexpr int kFewWaves = kDenseThreads / kWave, kFewLooks = 4;
+constexpr int kFewThreads = kDenseThreads, kFewWaves = kFewThreads / kWave, kFewLooks = kFewMost / kFewThreads;
+static_assert(kFewThreads == kFillThreads, "all threads of a block clear");
 
 // Clears the rows of the job that are not marked, as block number b of n (fill_share has the other case).
 __device__ __forceinline__ void fill_unmarked(const FillJob& j, const uint32_t* marks, int b, int n) {
@@ -393,19 +393,20 @@ __device__ __forceinline__ void fill_unmarked(const FillJob& j, const uint32_t* 
 }
 
 template <class TI, class TO, int VEC, bool ADD>
-__global__ __launch_bounds__(kDenseThreads) void k_dense_few(TableSource src, int B, uint32_t none,
-                                                             const TI* __restrict__ grad, int64_t ld_grad, int cols,
-                                                             int pieces, float scale, TO* __restrict__ out, int64_t ld,
-                                                             int clear, FillJob job) {
+__global__ __launch_bounds__(kFewThreads) void k_dense_few(TableSource src, int B, uint32_t none,
+                                                           const TI* __restrict__ grad, int64_t ld_grad, int cols,
+                                                           int pieces, float scale, TO* __restrict__ out, int64_t ld,
+                                                           int clear, FillJob job) {
   typedef typename Piece<TI, VEC>::V VI;
   extern __shared__ uint32_t marks[];
   __shared__ float part[kFewWaves - 1][VEC][kWave];
-  __shared__ uint16_t list[kFewWaves][kFewMost];
-  const int tid = threadIdx.x, lane = tid % kWave, w = tid / kWave;
+  __shared__ int counts[kFewWaves];
+  __shared__ uint16_t list[kFewMost];
+  const int tid = threadIdx.x, lane = tid % kWave, w = __builtin_amdgcn_readfirstlane(tid / kWave);
   if ((int)blockIdx.x < clear) {
-    for (int i = tid; i < (int)(none + 31) / 32; i += kDenseThreads) marks[i] = 0u;
+    for (int i = tid; i < (int)(none + 31) / 32; i += kFewThreads) marks[i] = 0u;
     __syncthreads();
-    for (int i = tid; i < B; i += kDenseThreads) {
+    for (int i = tid; i < B; i += kFewThreads) {
       const uint32_t id = key_of_id(src, i, none);
       if (id < none) atomicOr(&marks[id >> 5], 1u << (id & 31));
     }
@@ -417,24 +418,31 @@ __global__ __launch_bounds__(kDenseThreads) void k_dense_few(TableSource src, in
   const int at = (int)blockIdx.x - clear, b = at / slices, c = (at - b * slices) * kWave + lane;
   const uint32_t id = key_of_id(src, b, none);
   if (id >= none) return;
-  // the positions that have this id, in order: every wavefront keeps a list of its own
-  int count = 0;
-#pragma unroll 1
-  for (int i0 = 0; i0 < B; i0 += kFewLooks * kWave) {
-    uint32_t k[kFewLooks];
+  // the positions that have this id, in order: every wavefront looks through its part of them all
+  const int part_ids = (B + kFewWaves - 1) / kFewWaves, i0 = w * part_ids, i1 = min(i0 + part_ids, B);
+  unsigned long long same[kFewLooks];
+  int mine = 0;
 #pragma unroll
-    for (int m = 0; m < kFewLooks; ++m) k[m] = key_of_id(src, min(i0 + m * kWave + lane, B - 1), none);
-#pragma unroll
-    for (int m = 0; m < kFewLooks; ++m) {
-      const int i = i0 + m * kWave + lane;
-      const bool same = i < B && k[m] == id;
-      const unsigned long long all = __ballot(same);
-      if (same) list[w][count + __popcll(all & ((1ull << lane) - 1ull))] = (uint16_t)i;
-      count += __popcll(all);
-    }
+  for (int m = 0; m < kFewLooks; ++m) {
+    const int i = i0 + m * kWave + lane;
+    same[m] = __ballot(i < i1 && key_of_id(src, min(i, B - 1), none) == id);
+    mine += __popcll(same[m]);
   }
-  wave_sync();
-  if (list[w][0] != b) return;  // an earlier position has it
+  if (lane == 0) counts[w] = mine;
+  __syncthreads();
+  int count = 0, before = 0;
+#pragma unroll
+  for (int v = 0; v < kFewWaves; ++v) {
+    before += v < w ? counts[v] : 0;
+    count += counts[v];
+  }
+#pragma unroll
+  for (int m = 0; m < kFewLooks; ++m) {
+    if ((same[m] >> lane) & 1ull) list[before + __popcll(same[m] & ((1ull << lane) - 1ull))] = (uint16_t)(i0 + m * kWave + lane);
+    before += __popcll(same[m]);
+  }
+  __syncthreads();
+  if (list[0] != b) return;  // an earlier position has it
   const int waves = min((count + kDenseAhead - 1) / kDenseAhead, kFewWaves);  // that have rows to add
   const int col = piece_start<VEC>(min(c, pieces - 1), cols);
   float acc[VEC] = {};
@@ -444,10 +452,10 @@ __global__ __launch_bounds__(kDenseThreads) void k_dense_few(TableSource src, in
     auto ask = [&](VI(&v)[kDenseAhead], int from) {
 #pragma unroll
       for (int i = 0; i < kDenseAhead; ++i)
-        v[i] = __builtin_nontemporal_load((const VI*)(grad + (int64_t)list[w][min(from + i, count - 1)] * ld_grad + col));
+        v[i] = __builtin_nontemporal_load((const VI*)(grad + (int64_t)list[min(from + i, count - 1)] * ld_grad + col));
     };
     auto add = [&](const VI(&v)[kDenseAhead], int from) {
-      float eight[VEC] = {};  // summed by themselves: no value goes through more than 8 + 16 additions
+      float eight[VEC] = {};  // summed by themselves: no value goes through more than 8 + 32 + 4 additions
 #pragma unroll
       for (int i = 0; i < kDenseAhead; ++i) {
         if (from + i >= count) continue;
@@ -557,7 +565,7 @@ void launch_dense_few(const TableSource& src, int B, const tt_emb_matrix& grad, 
         const int pieces = (grad.cols + vec() - 1) / vec(), slices = (pieces + kWave - 1) / kWave;
         const int clear = add ? 0 : kFewClear, lds = add ? 0 : (int)((out.rows + 31) / 32 * 4);
         auto launch = [&](auto kernel) {
-          kernel<<<clear + B * slices, kDenseThreads, lds, st>>>(src, B, none, (const TI*)grad.data, grad.ld, grad.cols,
+          kernel<<<clear + B * slices, kFewThreads, lds, st>>>(src, B, none, (const TI*)grad.data, grad.ld, grad.cols,
                                                                  pieces, scale, (TO*)out.data, out.ld, clear, job);
         };
         if (add) launch(k_dense_few<TI, TO, vec(), true>);
@@ -621,13 +629,15 @@ void launch_dense_join(const DenseWork& ws, int sorted, int B, int tile, float s
                        hipStream_t st) {
   const uint32_t none = (uint32_t)out.rows;
   const int tiles = (B + tile - 1) / tile;
+  int lanes = 1;
+  while (lanes < kJoinLanes && lanes * 4 < out.cols) lanes *= 2;
   with_type(out.type, [&](auto to) {
     using TO = decltype(to);
     const dim3 grid((unsigned)std::min((tiles + kJoinTiles - 1) / kJoinTiles, 1 << 11),
                     (unsigned)(out.cols + kJoinCols - 1) / kJoinCols);
     auto launch = [&](auto kernel) {
       kernel<<<grid, kJoinThreads, 0, st>>>(ws.sort.key[sorted], B, tile, none, out.cols, scale, (TO*)out.data, out.ld,
-                                            ws.head, ws.tail, ws.stride, ws.starts);
+                                            ws.head, ws.tail, ws.stride, ws.starts, lanes);
     };
     if (add) launch(k_dense_join<TO, true>);
     else launch(k_dense_join<TO, false>);

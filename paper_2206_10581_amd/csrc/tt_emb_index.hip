@@ -454,17 +454,17 @@ __global__ __launch_bounds__(kScanThreads) void k_table_colscan(uint32_t* __rest
 }
 
 // Few ids of a plain table are sorted by their ranks alone, in one launch: the rank of a position is the number of
-// smaller keys, and of equal ones in front of it.  A block has G positions.  Its wavefronts share all keys, K times 64 of
-// them each, one a lane; a position's key is a scalar that a wavefront compares with its keys, and the lanes that
+// smaller keys, and of equal ones in front of it.  A block has 4 K positions, so that 256 blocks have
+// them all.  Its wavefronts share all keys, K times 64 of them each, one a lane; a position's key is a scalar that a wavefront compares with its keys, and the lanes that
 // are smaller are counted as one number: an instruction for 64 comparisons and two scalar ones, which bound it.  (With
 // positions in the lanes and keys from LDS 8192 ids took 11.6 us instead of 10.0.)  Blocks behind the first nblk clear
 // meanwhile.
 constexpr int kRankThreads = 1024, kRankWaves = kRankThreads / kWave;
-template <int G>
+template <int K>
 __global__ __launch_bounds__(kRankThreads) void k_table_rank(TableSource src, int B, uint32_t none,
                                                              uint32_t* __restrict__ key, uint32_t* __restrict__ pos,
                                                              int nblk, FillShare fill) {
-  constexpr int K = rank_most(G) / kRankThreads;
+  constexpr int G = 4 * K;
   __shared__ int counts[kRankWaves][G];
   if ((int)blockIdx.x >= nblk) {
     fill_share(fill, (int)blockIdx.x - nblk, (int)gridDim.x - nblk);
@@ -931,18 +931,23 @@ void launch_sort_pass(const Plan& pl, const Workspace& ws, const SortKeys& sk, c
 int launch_table_sort(const Workspace& ws, const SortKeys& sk, const TableSource& src, int B, const FillJob& job,
                       hipStream_t st) {
   const int clear = job.width != 0 ? kFillBlocks : 0;
-  // Sorting by ranks takes 10 us at 8192 ids and 32 at 16,384, by digits 22 at either; but a large job hides it, and
-  // has to be cut for the launches of the digits (1.05 GB beside 16,384 ids: 177 us in one launch, 216 in four).
-  if (B <= kRankMost || (B <= 2 * kRankMost && job.rows * job.width >= kFillLarge)) {
-    auto rank = [&](auto g) {
-      const int nblk = cdiv(B, g());
-      k_table_rank<g()><<<nblk + clear, kRankThreads, 0, st>>>(src, B, sk.sentinel, ws.key[0], ws.val[0], nblk,
+  // Sorting by ranks takes 10 us at 8192 ids, 18 at 12,288 and 32 at 16,384, by digits 22 at all; but a large job hides it,
+  // and has to be cut for the launches of the digits (1.05 GB beside 16,384 ids: 177 us in one launch, 216 in four).
+  if (B <= kRankMost || (B <= kRankMostLarge && job.rows * job.width >= kFillLarge)) {
+    auto rank = [&](auto k) {
+      const int nblk = cdiv(B, 4 * k());
+      k_table_rank<k()><<<nblk + clear, kRankThreads, 0, st>>>(src, B, sk.sentinel, ws.key[0], ws.val[0], nblk,
                                                                FillShare{job, 0, 1, 1});
     };
-    if (B <= rank_most(8)) rank(std::integral_constant<int, 8>{});
-    else if (B <= rank_most(16)) rank(std::integral_constant<int, 16>{});
-    else if (B <= rank_most(32)) rank(std::integral_constant<int, 32>{});
-    else rank(std::integral_constant<int, 64>{});
+    switch (cdiv(B, 2 * kRankThreads)) {
+      case 1: rank(std::integral_constant<int, 2>{}); break;
+      case 2: rank(std::integral_constant<int, 4>{}); break;
+      case 3: rank(std::integral_constant<int, 6>{}); break;
+      case 4: rank(std::integral_constant<int, 8>{}); break;
+      case 5: rank(std::integral_constant<int, 10>{}); break;
+      case 6: rank(std::integral_constant<int, 12>{}); break;
+      default: rank(std::integral_constant<int, 16>{}); break;
+    }
     return 0;
   }
   // shares of the job by what the launches take: about twice as long for a scatter as for the others

@@ -316,15 +316,15 @@ struct DenseWork {
   uint32_t* starts;  // per tile: the id whose long run starts in it, or none
 };
 // k_dense_few: most ids that are summed in one launch without a sort, beside a table of at most so many rows (a bit of
-// LDS for each) and bytes, and the blocks that clear it.  Against sort, sums and join, us: 129 ids in 32,000 x 512 bf16
-// 8.1 / 15.4, 512 there 10.6 / 17.5 (nine tenths of them the same 22.5 / 17.8), 129 in 32,001 x 2049 28 / 32, 512 in
-// 128,000 x 4096 225 / 176, where the rows' marks cost more than they save.  128 / 256 / 512 blocks: 14.0 / 9.8 / 8.1 at
-// the first.
-constexpr int kFewMost = 512, kFewClear = 512;
+// LDS for each) and bytes, and the blocks that clear it.  Against ranks, sums and joins, us: 129 ids in 32,000 x 512 bf16
+// 8.6 / 15.4, 512 there 10.6 / 17.5 (nine tenths of them the same 21.8 / 17.8), 1000 in 16,001 x 64 5.8 / 11.9, x 2048
+// 19.7 / 23.7, half of 1000 the same in 32,000 x 512 23.1 / 19.7; 512 in 128,000 x 4096 225 / 176, where the rows' marks
+// cost more than they save.  128 / 256 / 512 blocks: 14.0 / 9.8 / 8.1 at the first.
+constexpr int kFewMost = 1024, kFewClear = 512;
 constexpr int64_t kFewRows = 1 << 18, kFewBytes = 1 << 27;
-constexpr int kRankMost = 1 << 13;  // most ids that are sorted by k_table_rank, twice as many beside a large job
+constexpr int kRankMost = 3 << 12;  // most ids that are sorted by k_table_rank, and beside a large job
+constexpr int kRankMostLarge = 1 << 14;
 constexpr int64_t kFillLarge = int64_t(1) << 28;
-__host__ __device__ constexpr int rank_most(int positions) { return 256 * positions; }  // ids, by positions of a block
 constexpr int kDenseTileLeast = 8;  // fewest sorted slots of a tile (dense_tile)
 constexpr int kDenseAhead = 8;  // slots whose rows are under way at once
 

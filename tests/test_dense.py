@@ -142,7 +142,7 @@ def test_gradient_long_batches(B, dim, kind):
     _check(got, total, _bound(size, count, 1.0), "float32")
 
 
-@pytest.mark.parametrize("B", [1, 2, 8, 9, 33, 64, 65, 500, 512, 513])
+@pytest.mark.parametrize("B", [1, 2, 8, 9, 33, 64, 65, 500, 512, 513, 1023, 1024, 1025])
 @pytest.mark.parametrize("rows", [1, 7, 31, 32, 33, 1000, 262_144, 262_145])
 @pytest.mark.parametrize("how", ["uniform", "hot", "one", "none"])
 def test_gradient_of_few_positions(rows, B, how):
@@ -168,7 +168,8 @@ def test_gradient_of_few_positions(rows, B, how):
         assert (flat == 7.0).all()
 
 
-@pytest.mark.parametrize("B", [2048, 2049, 4096, 4097, 8192, 8193, 16_384, 16_385])
+@pytest.mark.parametrize("B", [1024, 1025, 2048, 2049, 4096, 4097, 6144, 6145, 8192, 8193, 10_240, 10_241, 12_288, 12_289,
+                               16_384, 16_385])
 @pytest.mark.parametrize("rows,dim", [(5003, 8), (2_900_001, 24)])
 def test_gradient_sorts(rows, dim, B):
     """Batch sizes at which another sort takes over, beside tables that are cleared quickly and slowly."""
