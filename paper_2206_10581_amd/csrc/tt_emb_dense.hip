@@ -584,6 +584,11 @@ void launch_fill(const FillJob& job, hipStream_t st) {
 // 13.9, 5003 of 1001 fp16 7.2 / 10.2 / 17.4, 50,000 of 24 fp32 8.3 / 13.1 / 19.8, 8192 of 2048 bf16 18.4 / 17.2 / 20.5,
 // 16,384 of 4096 bf16 45.8 / 43.1 / 45.4, 200,000 of 128 fp32 33.6 / 35.0 / 39.7.  Sums and joins together with 8 / 16:
 // 20,000 rows of 512 bf16 16.7 / 19.2, 65,536 of 256 23.1 / 21.4, 100,000 of 128 26.0 / 24.2.
+// Rows of fewer than 64 values: few are summed by a wavefront each all the same, many by groups of lanes.  All kernels of
+// a call in us, wavefronts / groups: 4295 ids, 8 bf16 values 15.2 / 18.6, 24 15.4 / 16.7, 56 16.7 / 18.5; 20,001 ids, 8
+// values 34.5 / 36.3, 56 35.3 / 37.2; 50,000, 24 fp32 values 43.0 / 38.1; 145,827, 8 bf16 values 56.5 / 57.5, 24 55.5 / 48.9,
+// 56 58.3 / 55.5.
+constexpr int kNarrowIds = 1 << 15;
 constexpr int64_t kTileFewPieces = (int64_t)64 << 16;
 constexpr int kTileFewIds = 1 << 16;
 int dense_tile(int B, int cols, int type) {
@@ -619,7 +624,7 @@ void launch_dense_sum(const DenseWork& ws, int sorted, int B, const tt_emb_matri
         if (add) launch(k_dense_sum<TI, TO, vec(), true, wave()>, ln);
         else launch(k_dense_sum<TI, TO, vec(), false, wave()>, ln);
       };
-      if (grad.cols >= kWave) with_wave_piece<TI>(grad.cols, [&](auto vec) { sums(vec, std::true_type{}); });
+      if (grad.cols >= kWave || B <= kNarrowIds) with_wave_piece<TI>(grad.cols, [&](auto vec) { sums(vec, std::true_type{}); });
       else with_piece<TI>(grad.cols, [&](auto vec) { sums(vec, std::false_type{}); });
     });
   });

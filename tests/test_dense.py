@@ -128,7 +128,8 @@ def test_gradient_runs(rows, B, how):
     assert torch.equal(got, emb.backward(torch.from_numpy(ids).cuda(), grad))     # a fixed order
 
 
-@pytest.mark.parametrize("B,dim,kind", [(65_535, 72, "bfloat16"), (65_536, 65, "float32"), (70_000, 480, "bfloat16"),
+@pytest.mark.parametrize("B,dim,kind", [(32_768, 3, "float16"), (32_768, 24, "bfloat16"), (32_769, 3, "float16"),
+                                        (32_769, 24, "bfloat16"), (32_769, 63, "float32"), (65_535, 72, "bfloat16"), (65_536, 65, "float32"), (70_000, 480, "bfloat16"),
                                         (140_001, 8, "float32"), (530_003, 4, "bfloat16")])
 def test_gradient_long_batches(B, dim, kind):
     import torch
