@@ -220,10 +220,10 @@ __global__ __launch_bounds__(kDenseThreads) void k_dense_sum(const uint32_t* __r
 }
 
 // Long runs: the parts that their tiles left are added in a fixed order.  A block looks at 64 tiles and takes 128
-// columns; a lane has four of them, and the halves (of narrower rows smaller parts) of a wavefront take a run's
-// parts in turn.  A wavefront takes a run of its own, but all of them the one run of a block that has more than 64 parts.  65,536 ids, half of
-// them the same, rows of 1024 bf16: 88 us with four wavefronts on every run and its end looked for from 64 tiles to
-// the next 64, 25 so.  64 columns a block take 17 there, but 15 instead of 9 at 16,384 rows of 4096.
+// columns; a lane has four of them, and the halves (of narrower rows smaller parts) of a wavefront take a run's parts in
+// turn.  A wavefront takes a run of its own, but all of them the one run of a block that has more than 64 parts.  65,536
+// ids, half of them the same, rows of 1024 bf16: 88 us with four wavefronts on every run and its end looked for from 64
+// tiles to the next 64, 25 so.  64 columns a block take 17 there, but 15 instead of 9 at 16,384 rows of 4096.
 constexpr int kJoinThreads = 1024, kJoinWaves = kJoinThreads / kWave, kJoinTiles = kWave, kJoinCols = 128;
 constexpr int kJoinLanes = kJoinCols / 4;  // at most
 constexpr int kJoinAhead = 8;  // parts under way at once
@@ -624,8 +624,10 @@ void launch_dense_sum(const DenseWork& ws, int sorted, int B, const tt_emb_matri
         if (add) launch(k_dense_sum<TI, TO, vec(), true, wave()>, ln);
         else launch(k_dense_sum<TI, TO, vec(), false, wave()>, ln);
       };
-      if (grad.cols >= kWave || B <= kNarrowIds) with_wave_piece<TI>(grad.cols, [&](auto vec) { sums(vec, std::true_type{}); });
-      else with_piece<TI>(grad.cols, [&](auto vec) { sums(vec, std::false_type{}); });
+      if (grad.cols >= kWave || B <= kNarrowIds)
+        with_wave_piece<TI>(grad.cols, [&](auto vec) { sums(vec, std::true_type{}); });
+      else
+        with_piece<TI>(grad.cols, [&](auto vec) { sums(vec, std::false_type{}); });
     });
   });
 }

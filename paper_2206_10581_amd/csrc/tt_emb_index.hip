@@ -454,11 +454,11 @@ __global__ __launch_bounds__(kScanThreads) void k_table_colscan(uint32_t* __rest
 }
 
 // Few ids of a plain table are sorted by their ranks alone, in one launch: the rank of a position is the number of
-// smaller keys, and of equal ones in front of it.  A block has 4 K positions, so that 256 blocks have
-// them all.  Its wavefronts share all keys, K times 64 of them each, one a lane; a position's key is a scalar that a wavefront compares with its keys, and the lanes that
-// are smaller are counted as one number: an instruction for 64 comparisons and two scalar ones, which bound it.  (With
-// positions in the lanes and keys from LDS 8192 ids took 11.6 us instead of 10.0.)  Blocks behind the first nblk clear
-// meanwhile.
+// smaller keys, and of equal ones in front of it.  A block has 4 K positions, so that 256 blocks have them all.  Its
+// wavefronts share all keys, K times 64 of them each, one a lane; a position's key is a scalar that a wavefront compares
+// with its keys, and the lanes that are smaller are counted as one number: an instruction for 64 comparisons and two
+// scalar ones, which bound it.  (With positions in the lanes and keys from LDS 8192 ids took 11.6 us instead of 10.0.)
+// Blocks behind the first nblk clear meanwhile.
 constexpr int kRankThreads = 1024, kRankWaves = kRankThreads / kWave;
 template <int K>
 __global__ __launch_bounds__(kRankThreads) void k_table_rank(TableSource src, int B, uint32_t none,
