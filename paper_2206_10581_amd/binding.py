@@ -547,8 +547,9 @@ class GradientClip(_OnDevice):
     """The 2-norm over all values of many tensors, and the tensors scaled to a largest norm.
 
     tensors: on one GPU, float32, bfloat16 or float16, each without gaps (any order of dimensions), not overlapping
-    each other; borrowed.  out: tensors of the same sizes, in any of the types, that receive the scaled
-    values; None: in place.  Must not be used from two threads or streams at once."""
+    each other; borrowed, with the memory that they have now (make a new object for tensors whose .data is replaced).
+    out: tensors of the same sizes, in any of the types, that receive the scaled values; None: in place.  Must not be used
+    from two threads or streams at once."""
 
     def __init__(self, tensors, out=None):
         self.tensors = list(tensors)
@@ -556,6 +557,7 @@ class GradientClip(_OnDevice):
             raise ValueError("no tensors")
         super().__init__(self.tensors[0].device)
         self._in = self._values(self.tensors)
+        self._held = [t.detach() for t in self.tensors]  # their memory stays if .data is replaced
         self.out, self._out = None, None
         if out is not None:
             self.out = list(out)
@@ -564,6 +566,7 @@ class GradientClip(_OnDevice):
             if any(a.stride() != b.stride() for a, b in zip(self.tensors, self.out) if a.numel() > 1):
                 raise ValueError("out: tensors of the same strides needed")
             self._out = self._values(self.out)
+            self._held += [t.detach() for t in self.out]
         rc, nbytes = tt_emb_norm_workspace_bytes(len(self.tensors))
         if rc:
             raise TTEmbError(rc, "tt_emb_norm_workspace_bytes")

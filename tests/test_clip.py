@@ -186,3 +186,16 @@ def test_refusals():
                 lambda: clip.norm(scale=float("inf")), lambda: clip.clip(1.0, scale=float("nan"))):
         with pytest.raises(tt.TTEmbError):
             bad()
+
+
+def test_the_memory_of_replaced_tensors_is_held():
+    """The object works on the memory that the tensors had when it was made, which is not given to others."""
+    import torch
+    import paper_2206_10581_amd as tt
+    x, y = torch.full((100_000,), 3.0, device="cuda"), torch.zeros(100_000, device="cuda")
+    clip = tt.GradientClip([x], out=[y])
+    x.data, y.data = torch.zeros(1, device="cuda"), torch.zeros(1, device="cuda")
+    others = [torch.full((100_000,), 7.0, device="cuda") for _ in range(4)]
+    want = 3.0 * 100_000 ** 0.5
+    assert abs(clip.clip(1.0).item() - want) <= want * 2.0 ** -23
+    assert all(bool((t == 7.0).all()) for t in others)
