@@ -436,7 +436,6 @@ class _OnDevice:
         # the handle alone where torch gives it: making a stream object takes 1 us of a call's 7
         self._stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
             lambda index: torch.cuda.current_stream(index).cuda_stream)
-        self._home = self._stream(self.index)  # the workspace belongs to this stream
 
     def _call(self, function, *args):
         """The C function with the current stream of this object's device as its last argument."""
@@ -463,6 +462,7 @@ class _OnDevice:
         raise ValueError(f"type {kind}: float32, bfloat16 or float16 needed")
 
     def _make_workspace(self, nbytes):
+        self._home = self._stream(self.index)  # the workspace belongs to this stream
         self.workspace = self.torch.empty(nbytes + 256, dtype=self.torch.uint8, device=self.device)
         self._ws_ptr = (self.workspace.data_ptr() + 255) & ~255
         self.workspace_bytes = nbytes
@@ -472,21 +472,16 @@ class DenseEmbedding(_OnDevice):
     """A table kept as a plain matrix, beside tensor-train ones: lookup times a scale, and gradient.
 
     weight: [rows, dim] on the GPU, float32, bfloat16 or float16, values of a row side by side (rows may lie further
-    apart); borrowed.  Ids outside the table give zero rows and no gradient; padding_id is an id that has a
-    row but no gradient.  Must not be used from two threads or streams at once (the workspace of backward)."""
+    apart); borrowed, and taken with the memory, shape, strides and type that it has at the time of a call.  Ids outside
+    the table give zero rows and no gradient; padding_id is an id that has a row but no gradient.  Outputs must not
+    overlap what a call reads.  Must not be used from two threads or streams at once (the workspace of backward)."""
 
     def __init__(self, weight, max_batch: int, scale: float = 1.0, padding_id: int | None = None):
         super().__init__(weight.device)
         self.weight, self.max_batch, self.scale = weight, int(max_batch), float(scale)
         self.padding_id = -1 if padding_id is None else int(padding_id)
-        self._table = self._matrix(weight)
-        self.rows, self.dim = weight.shape
-        if self.dim < 1:
-            raise ValueError("rows without values")
-        rc, nbytes = tt_emb_dense_workspace_bytes(self.dim, self.max_batch)
-        if rc:
-            raise TTEmbError(rc, "tt_emb_dense_workspace_bytes")
-        self._make_workspace(nbytes)
+        self._described, self._table, self._spaces, self.workspace_bytes = None, None, [], 0
+        self._weight()
 
     def _matrix(self, t):
         if t.dim() != 2 or t.device != self.device:
@@ -504,30 +499,53 @@ class DenseEmbedding(_OnDevice):
             raise TTEmbError(TT_EMB_ENOSPC, "DenseEmbedding")
         return ids.data_ptr()
 
+    @property
+    def rows(self):
+        return self.weight.shape[0]
+
+    @property
+    def dim(self):
+        return self.weight.shape[1]
+
     def _weight(self):
-        if self.weight.data_ptr() != self._table.data:  # the parameter's storage was replaced
-            self._table = self._matrix(self.weight)
+        """The weight as it is now.  Its address alone does not tell: a view of the same memory may have other rows,
+        and a freed address may be given to a smaller tensor of another type."""
+        w = self.weight
+        now = (w.data_ptr(), w.dtype, w.shape, w.stride())
+        if now != self._described:
+            table = self._matrix(w)
+            if table.cols < 1:
+                raise ValueError("rows without values")
+            rc, nbytes = tt_emb_dense_workspace_bytes(table.cols, self.max_batch)
+            if rc:
+                raise TTEmbError(rc, "tt_emb_dense_workspace_bytes")
+            if nbytes > self.workspace_bytes:
+                self._make_workspace(nbytes)
+                self._spaces.append(self.workspace)  # a captured graph may go on using a smaller one
+            self._table, self._described = table, now
         return self._table
 
     def forward(self, ids, out=None, dtype=None):
         """scale * weight[ids], in the weight's type unless out or dtype says otherwise."""
-        ptr = self._ids(ids)
+        table, ptr = self._weight(), self._ids(ids)
         if out is None:
-            out = self.torch.empty((ids.numel(), self.dim), dtype=dtype or self.weight.dtype, device=self.device)
-        elif out.shape != (ids.numel(), self.dim) or dtype not in (None, out.dtype):
-            raise ValueError(f"out: {(ids.numel(), self.dim)} of {dtype or out.dtype} needed, not {tuple(out.shape)}")
-        self._call(self.lib.tt_emb_dense_forward, byref(self._weight()), ptr, self.scale, byref(self._matrix(out)))
+            out = self.torch.empty((ids.numel(), table.cols), dtype=dtype or self.weight.dtype, device=self.device)
+        elif out.shape != (ids.numel(), table.cols) or dtype not in (None, out.dtype):
+            raise ValueError(f"out: {(ids.numel(), table.cols)} of {dtype or out.dtype} needed, not {tuple(out.shape)}")
+        self._call(self.lib.tt_emb_dense_forward, byref(table), ptr, self.scale, byref(self._matrix(out)))
         return out
 
     def backward(self, ids, grad_out, out=None, dtype=None, add: bool = False):
         """Gradient of forward(ids) with respect to the weight, [rows, dim], for the upstream gradient grad_out.
         With add, it is added to out, whose other rows are left alone."""
+        table = self._weight()
+        shape = (table.rows, table.cols)
         if out is None:
             if add:
                 raise ValueError("add needs out")
-            out = self.torch.empty((self.rows, self.dim), dtype=dtype or self.weight.dtype, device=self.device)
-        elif out.shape != (self.rows, self.dim) or dtype not in (None, out.dtype):
-            raise ValueError(f"out: {(self.rows, self.dim)} of {dtype or out.dtype} needed, not {tuple(out.shape)}")
+            out = self.torch.empty(shape, dtype=dtype or self.weight.dtype, device=self.device)
+        elif out.shape != shape or dtype not in (None, out.dtype):
+            raise ValueError(f"out: {shape} of {dtype or out.dtype} needed, not {tuple(out.shape)}")
         self._backward(ids, grad_out, self.scale, self._matrix(out), add)
         return out
 
@@ -537,8 +555,8 @@ class DenseEmbedding(_OnDevice):
 
     def _backward(self, ids, grad_out, scale, target, add):
         ptr = self._ids(ids)
-        if grad_out.shape != (ids.numel(), self.dim):
-            raise ValueError(f"grad_out: {(ids.numel(), self.dim)} needed, not {tuple(grad_out.shape)}")
+        if grad_out.shape != (ids.numel(), target.cols):
+            raise ValueError(f"grad_out: {(ids.numel(), target.cols)} needed, not {tuple(grad_out.shape)}")
         self._call(self.lib.tt_emb_dense_backward, ptr, byref(self._matrix(grad_out)), scale, self.padding_id, byref(target),
                    1 if add else 0, self._ws_ptr, self.workspace_bytes)
 
