@@ -320,10 +320,11 @@ int tt_emb_grad_norm(const tt_emb_values* in, int32_t n, float scale, float* nor
 
 /*
  * The same norm, and the tensors scaled so that theirs is at most max_norm:
- *   out[i] = in[i] * (scale * c),   c = min(1, max_norm / (*norm + eps)),
+ *   out[i] = in[i] * (scale * c),   c = min(1, max_norm / (*norm + eps)),   c = 1 where *norm + eps <= max_norm,
  * formed in fp64, rounded to fp32 and then to the output's type.  out: tensors of the same counts and any types, or NULL for in place; an output may be
  * its own input (same address and type) and overlaps no other.  In place with scale * c = 1 nothing is written.  A norm
- * that is infinite or not a number is not hidden: c is 0 (and infinities become NaN) or NaN.  max_norm >= 0, eps >= 0.
+ * that is infinite or not a number is not hidden: c is 0 (and infinities become NaN) under a finite max_norm, or NaN.
+ * max_norm >= 0 (infinite: no limit), eps >= 0.
  */
 int tt_emb_grad_clip(const tt_emb_values* in, const tt_emb_values* out, int32_t n, float scale, float max_norm,
                      float eps, float* norm, void* workspace, size_t workspace_bytes, void* hip_stream);

@@ -206,8 +206,8 @@ __device__ __forceinline__ void scale_unit(const ITEMS& items, int a, int64_t u,
 }
 
 __device__ __forceinline__ double clip_factor(double norm, float scale, float max_norm, float eps) {
-  const double ratio = (double)max_norm / (norm + (double)eps);
-  return (double)scale * (ratio >= 1.0 ? 1.0 : ratio);  // NaN stays
+  const double n = norm + (double)eps, most = (double)max_norm;
+  return (double)scale * (n <= most ? 1.0 : most / n);  // 0 / 0 and inf / inf are within the limit; NaN stays
 }
 
 // Every block adds up the parts of the norm, which costs it less than a launch in between.
