@@ -581,7 +581,8 @@ class GradientClip(_OnDevice):
             self.out = list(out)
             if [t.shape for t in self.out] != [t.shape for t in self.tensors]:
                 raise ValueError("out: tensors of the same shapes needed")
-            if any(a.stride() != b.stride() for a, b in zip(self.tensors, self.out) if a.numel() > 1):
+            if any(a.stride() != b.stride() and self._order(a) != self._order(b) for a, b in zip(self.tensors, self.out)
+                   if a.numel() > 1):
                 raise ValueError("out: tensors of the same strides needed")
             self._out = self._values(self.out)
             self._held += [t.detach() for t in self.out]
@@ -599,6 +600,10 @@ class GradientClip(_OnDevice):
                 raise ValueError(f"tensor of shape {tuple(t.shape)} and strides {t.stride()} has gaps or overlaps")
             v.data, v.count, v.type = t.data_ptr(), t.numel(), self._type(t)
         return values
+
+    @staticmethod
+    def _order(t):
+        return [s for s, n in zip(t.stride(), t.shape) if n > 1]  # the others say nothing
 
     @staticmethod
     def _dense(t):

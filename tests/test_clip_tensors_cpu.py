@@ -1,0 +1,38 @@
+"""Which tensors GradientClip takes.  The wrapper's own code runs on tensors in host memory; its calls of the library are
+recorded and none is made."""
+import pytest
+import torch
+
+from paper_2206_10581_amd import binding as b
+
+
+@pytest.fixture
+def made(monkeypatch):
+    """Makes GradientClips on the host; the names of the functions that they call are left in `made.calls`."""
+    def init(self, device):
+        self.torch, self.device, self.index, self.lib = torch, device, 0, b.load_library()
+        self._stream = lambda index: 0
+        self._home = 0
+
+    def made(tensors, out=None):
+        return b.GradientClip(tensors, out=out)
+
+    made.calls = []
+    monkeypatch.setattr(b._OnDevice, "__init__", init)
+    monkeypatch.setattr(b._OnDevice, "_call", lambda self, function, *args: made.calls.append(function.__name__))
+    return made
+
+
+def test_strides_of_single_places_do_not_matter(made):
+    """Weights of 1 x 1 convolutions: the two orders of dimensions are one order of values."""
+    a = torch.zeros(64, 3, 1, 1)
+    for other in (a.to(memory_format=torch.channels_last), a.as_strided((64, 3, 1, 1), (3, 1, 99, 7)),
+                  torch.empty_strided((64, 3, 1, 1), (3, 1, 1, 192))):
+        made([a], [other.clone(memory_format=torch.preserve_format)])
+        made([other], [torch.zeros(64, 3, 1, 1)])
+    one, several = torch.zeros(1, 5), torch.zeros(4, 5)[::4]
+    assert one.stride() == (5, 1) and several.stride() == (20, 1)
+    made([one], [several])
+    for bad in (torch.zeros(3, 64, 1, 1).permute(1, 0, 2, 3), torch.zeros(64, 6, 1, 1)[:, ::2], torch.zeros(64, 1, 1, 3).permute(0, 3, 1, 2)[:, :, :, :0]):
+        with pytest.raises(ValueError):
+            made([a], [bad])
