@@ -26,6 +26,7 @@ class TTEmbConfig(ctypes.Structure):
 
 
 TT_EMB_FP32, TT_EMB_BF16, TT_EMB_FP16 = 0, 1, 2
+_TYPE_BYTES = (4, 2, 2)
 
 
 class TTEmbMatrix(ctypes.Structure):
@@ -564,17 +565,18 @@ class DenseEmbedding(_OnDevice):
 class GradientClip(_OnDevice):
     """The 2-norm over all values of many tensors, and the tensors scaled to a largest norm.
 
-    tensors: on one GPU, float32, bfloat16 or float16, each without gaps (any order of dimensions), not overlapping
-    each other; borrowed, with the memory that they have now (make a new object for tensors whose .data is replaced).
-    out: tensors of the same sizes, in any of the types, that receive the scaled values; None: in place.  Must not be used
-    from two threads or streams at once."""
+    tensors: on one GPU, float32, bfloat16 or float16, each without gaps (any order of dimensions); borrowed, with the
+    memory that they have now (make a new object for tensors whose .data is replaced).  out: tensors of the same sizes,
+    in any of the types, that receive the scaled values; None: in place.  What clip writes may overlap nothing but its
+    own input.  Must not be used from two threads or streams at once."""
 
     def __init__(self, tensors, out=None):
         self.tensors = list(tensors)
         if not self.tensors:
             raise ValueError("no tensors")
         super().__init__(self.tensors[0].device)
-        self._in = self._values(self.tensors)
+        self._in, read = self._values(self.tensors)
+        written = read
         self._held = [t.detach() for t in self.tensors]  # their memory stays if .data is replaced
         self.out, self._out = None, None
         if out is not None:
@@ -584,22 +586,45 @@ class GradientClip(_OnDevice):
             if any(a.stride() != b.stride() and self._order(a) != self._order(b) for a, b in zip(self.tensors, self.out)
                    if a.numel() > 1):
                 raise ValueError("out: tensors of the same strides needed")
-            self._out = self._values(self.out)
+            self._out, written = self._values(self.out)
             self._held += [t.detach() for t in self.out]
+        self._apart = self._written_apart(read, written)
+        if out is not None and not self._apart:
+            raise ValueError("out: tensors that overlap nothing but each its own input needed")
         rc, nbytes = tt_emb_norm_workspace_bytes(len(self.tensors))
         if rc:
             raise TTEmbError(rc, "tt_emb_norm_workspace_bytes")
         self._make_workspace(nbytes)
 
     def _values(self, tensors):
-        values = (TTEmbValues * len(tensors))()
+        """The tensors as the library takes them, and the (start, end, type) of each in memory."""
+        values, spans = (TTEmbValues * len(tensors))(), []
         for v, t in zip(values, tensors):
             if t.device != self.device:
                 raise ValueError(f"tensor on {t.device}, not {self.device}")
             if not (t.is_contiguous() or self._dense(t)):
                 raise ValueError(f"tensor of shape {tuple(t.shape)} and strides {t.stride()} has gaps or overlaps")
-            v.data, v.count, v.type = t.data_ptr(), t.numel(), self._type(t)
-        return values
+            at, count, kind = t.data_ptr(), t.numel(), self._type(t)
+            v.data, v.count, v.type = at, count, kind
+            spans.append((at, at + count * _TYPE_BYTES[kind], kind))
+        return values, spans
+
+    @staticmethod
+    def _written_apart(read, written):
+        """Whether clip writes every value's place once and reads none that it writes elsewhere."""
+        spans = [(start, end, True) for start, end, _ in written if start < end]
+        if read is not written:
+            spans += [(start, end, False) for (start, end, kind), to in zip(read, written)
+                      if start < end and (start, end, kind) != to]
+        read_to = written_to = 0
+        for start, end, writes in sorted(spans):
+            if start < written_to or writes and start < read_to:
+                return False
+            if writes:
+                written_to = end
+            elif end > read_to:
+                read_to = end
+        return True
 
     @staticmethod
     def _order(t):
@@ -630,6 +655,8 @@ class GradientClip(_OnDevice):
 
     def clip(self, max_norm: float, scale: float = 1.0, eps: float = 1e-6, out=None):
         """Scales the tensors by scale and down to max_norm; returns the norm before, |scale| included."""
+        if not self._apart:
+            raise ValueError("tensors that overlap cannot be scaled in place")
         out = self._norm(out)
         self._call(self.lib.tt_emb_grad_clip, self._in, self._out, len(self._in), float(scale), float(max_norm), float(eps),
                    out.data_ptr(), self._ws_ptr, self.workspace_bytes)

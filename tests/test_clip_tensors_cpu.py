@@ -36,3 +36,33 @@ def test_strides_of_single_places_do_not_matter(made):
     for bad in (torch.zeros(3, 64, 1, 1).permute(1, 0, 2, 3), torch.zeros(64, 6, 1, 1)[:, ::2], torch.zeros(64, 1, 1, 3).permute(0, 3, 1, 2)[:, :, :, :0]):
         with pytest.raises(ValueError):
             made([a], [bad])
+
+
+def test_tensors_that_overlap_are_not_scaled(made):
+    """Several blocks would scale the same values, some of them twice; their norm is well defined."""
+    x = torch.zeros(1000)
+    for tensors in ([x, x], [x[:5], x], [x[:501], x[500:]], [x[10:20], x[:5], x[19:40]], [x, x.view(torch.bfloat16)]):
+        clip = made(tensors)
+        clip.norm()
+        for _ in range(2):
+            with pytest.raises(ValueError):
+                clip.clip(1.0)
+        assert made.calls.pop() == "tt_emb_grad_norm" and not made.calls
+        made(tensors, [torch.zeros_like(t) for t in tensors]).clip(1.0)      # read twice, written once each
+        made.calls.clear()
+    for tensors in ([x[:500], x[500:]], [x[500:], x[:500], x[3:3], x[3:3]], [x[::2][:1], x[1:]], [x]):
+        made(tensors).clip(1.0)
+
+
+def test_outputs_overlap_nothing_but_their_own_inputs(made):
+    x, y, z = torch.zeros(1000), torch.zeros(1000), torch.zeros(1000)
+    half = torch.zeros(1000, dtype=torch.bfloat16)
+    for tensors, out in (([x, y], [z, z]), ([x, y], [y, x]), ([x[:99], y[:99]], [x[1:100], y[:99]]), ([x, y], [y, z]),
+                         ([half], [half.view(torch.float16)]), ([x[:500].view(torch.bfloat16)], [x]),
+                         ([x, x], [x, y]), ([x, x[:9]], [x, y[:9]])):
+        with pytest.raises(ValueError):
+            made(tensors, out)
+    for tensors, out in (([x, y], [x, y]), ([x, y], [x, z]), ([x[:5], x[5:9]], [z[4:9], z[:4]]), ([x, x[:7]], [y, z[:7]]),
+                         ([x[:500], x[500:]], [x[:500], y[:500]]), ([half], [x]), ([x[7:7]], [x[7:7]])):
+        made(tensors, out).clip(1.0)
+    assert len(made.calls) == 7
