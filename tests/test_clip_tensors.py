@@ -27,3 +27,28 @@ def test_overlapping_tensors_have_a_norm_but_are_not_scaled():
     assert (x == 3.0).all()
     tt.GradientClip([x, x], out=[x.clone(), y]).clip(3.0 * 200 ** 0.5 / 2, eps=0.0)
     assert (y == 1.5).all()
+
+
+def test_memory_that_was_freed_is_not_written():
+    import torch
+    import paper_2206_10581_amd as tt
+    x, y = torch.full((100_000,), 3.0, device="cuda"), torch.zeros(50, device="cuda")
+    clip = tt.GradientClip([y, x])
+    clip.clip(1e9)
+    x.untyped_storage().resize_(0)
+    others = [torch.full((100_000,), 7.0, device="cuda") for _ in range(4)]
+    for call in (lambda: clip.norm(), lambda: clip.clip(1.0)):
+        with pytest.raises(RuntimeError):
+            call()
+    assert all(bool((t == 7.0).all()) for t in others)
+
+
+def test_a_replaced_tensor_is_told():
+    import torch
+    import paper_2206_10581_amd as tt
+    x = torch.full((4096,), 3.0, device="cuda")
+    clip = tt.GradientClip([x])
+    x.data = torch.zeros(4096, device="cuda")
+    with pytest.warns(RuntimeWarning, match="replaced"):
+        assert clip.clip(1.0).item() == 192.0
+    assert not x.any() and tt.GradientClip([x]).norm().item() == 0.0

@@ -66,3 +66,60 @@ def test_outputs_overlap_nothing_but_their_own_inputs(made):
                          ([x[:500], x[500:]], [x[:500], y[:500]]), ([half], [x]), ([x[7:7]], [x[7:7]])):
         made(tensors, out).clip(1.0)
     assert len(made.calls) == 7
+
+
+def test_freed_memory_is_not_touched(made):
+    """The memory of a tensor is its storage's: held by the object, but given back where the storage itself is resized."""
+    for k in range(4):
+        tensors, outs = [torch.zeros(50), torch.zeros(60)], [torch.zeros(50), torch.zeros(60)]
+        clip = made(tensors, outs)
+        clip.clip(1.0)
+        t = (tensors + outs)[k]
+        made.calls.clear()
+        t.untyped_storage().resize_(0)
+        for call in (lambda: clip.norm(), lambda: clip.clip(1.0)):
+            with pytest.raises(RuntimeError):
+                call()
+        t.untyped_storage().resize_(100_000)          # somewhere else
+        with pytest.raises(RuntimeError):
+            clip.clip(1.0)
+        assert not made.calls
+        made(tensors, outs).clip(1.0)
+
+
+def test_a_replaced_tensor_is_told(made):
+    """The object goes on with the memory that its tensors had, and says so."""
+    import warnings
+    for k in range(4):
+        tensors, outs = [torch.zeros(50), torch.zeros(60)], [torch.zeros(50), torch.zeros(60)]
+        clip = made(tensors, outs)
+        with warnings.catch_warnings():
+            warnings.simplefilter("error")
+            clip.norm()
+            clip.clip(1.0)
+        t = (tensors + outs)[k]
+        t.data = torch.zeros_like(t)
+        made.calls.clear()
+        with pytest.warns(RuntimeWarning, match="replaced"):
+            clip.norm()
+        with pytest.warns(RuntimeWarning, match="replaced"):
+            clip.clip(1.0)
+        assert made.calls == ["tt_emb_grad_norm", "tt_emb_grad_clip"]
+        clip._held[k].untyped_storage().resize_(0)    # and what was held is gone too
+        with pytest.raises(RuntimeError):
+            clip.clip(1.0)
+
+
+def test_views_of_one_buffer_are_watched_as_one(made):
+    flat, other = torch.zeros(1000), torch.zeros(30)
+    tensors = [flat[:10], flat[10:10], other, flat[500:], other[:0], flat[20:500]]
+    clip = made(tensors)
+    assert len(clip._watched) == 2
+    clip.clip(1.0)
+    tensors[5].data = torch.zeros(480)
+    clip.clip(1.0)                                    # on the buffer, which is held
+    flat.untyped_storage().resize_(0)
+    with pytest.raises(RuntimeError):
+        clip.norm()
+    del flat, other, tensors[:]
+    assert clip._held[1].numel() == 30
