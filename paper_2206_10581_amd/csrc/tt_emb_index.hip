@@ -932,7 +932,8 @@ int launch_table_sort(const Workspace& ws, const SortKeys& sk, const TableSource
                       hipStream_t st) {
   const int clear = job.width != 0 ? kFillBlocks : 0;
   // Sorting by ranks takes 10 us at 8192 ids, 18 at 12,288 and 32 at 16,384, by digits 22 at all; but a large job hides it,
-  // and has to be cut for the launches of the digits (1.05 GB beside 16,384 ids: 177 us in one launch, 216 in four).
+  // and has to be cut for the launches of the digits (1.05 GB beside 16,384 ids: 177 us in one launch, 216 in four).  More
+  // than 16,384 go by digits beside a large job too: a block of ranks has no lanes for more positions.
   if (B <= kRankMost || (B <= kRankMostLarge && job.rows * job.width >= kFillLarge)) {
     auto rank = [&](auto k) {
       const int nblk = cdiv(B, 4 * k());

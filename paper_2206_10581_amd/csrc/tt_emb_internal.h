@@ -322,7 +322,9 @@ struct DenseWork {
 // cost more than they save.  128 / 256 / 512 blocks: 14.0 / 9.8 / 8.1 at the first.
 constexpr int kFewMost = 1024, kFewClear = 512;
 constexpr int64_t kFewRows = 1 << 18, kFewBytes = 1 << 27;
-constexpr int kRankMost = 3 << 12;  // most ids that are sorted by k_table_rank, and beside a large job
+// Most ids that are sorted by k_table_rank, and beside a large job.  The second is the kernel's own end: with K = 16 a
+// thread has that many keys and a block 4 K = 64 positions, one for every lane of a wavefront.
+constexpr int kRankMost = 3 << 12;
 constexpr int kRankMostLarge = 1 << 14;
 constexpr int64_t kFillLarge = int64_t(1) << 28;
 constexpr int kDenseTileLeast = 8;  // fewest sorted slots of a tile (dense_tile)

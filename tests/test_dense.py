@@ -1,10 +1,12 @@
 """Plain tables: lookup with a scale and gradient by sorted ids, against plain sums in 64 bits.
 
 Tolerances.  u(type) is half a unit of the last place of 1: 2^-24 for fp32, 2^-8 for bf16, 2^-11 for fp16.  A lookup is
-one product in fp32 and one rounding to the output's type: relative error 2^-24 + u.  A sum of m values is cut into tiles
-of 32 sorted positions, a tile that finishes its last run adds up at most 64, and the parts are added one after the
-other: at most 64 + m/32 additions in fp32 touch a value, each with relative error 2^-24, then come the scale (2^-24)
-and the output's rounding."""
+one product in fp32 and one rounding to the output's type: relative error 2^-24 + u.  A sum of m values: up to 1024
+positions are added by eights, at most 8 + 32 + 4 additions in fp32 touching a value.  More are cut into tiles of 8 or 16
+sorted positions, of which a tile adds up at most 32; the parts of a longer run, m/8 and two more, are added one after
+the other by two groups of lanes (of more than 64 parts by 32 groups) and joined in 6 + 15 more.  The tests allow
+64 + m/32 additions, which is no fewer: 32 + (m/16 + 1) + 6 to 496 positions, 32 + 32 + 6 to where 64 parts end, and
+32 + (m/256 + 1) + 21 beyond.  Each has relative error 2^-24; then come the scale (2^-24) and the output's rounding."""
 import numpy as np
 import pytest
 
