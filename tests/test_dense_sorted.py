@@ -44,6 +44,10 @@ def _sums(ids, grad, rows, padding=-1):
     import torch
     keep = torch.nonzero((ids >= 0) & (ids < rows) & (ids != padding))[:, 0]
     at, g = ids[keep], grad[keep].double()
+    if len(ids) > 1_000_000:       # on the host: additions into one row wait for each other on the GPU
+        columns = [[np.bincount(at.cpu(), weights=c, minlength=rows) for c in m.t().cpu().numpy()] for m in (g, g.abs())]
+        total, size = (torch.from_numpy(np.stack(c, 1)).cuda() for c in columns)
+        return total, size, torch.bincount(at, minlength=rows).double()[:, None]
     total = torch.zeros(rows, grad.shape[1], dtype=torch.float64, device="cuda").index_add_(0, at, g)
     size = torch.zeros_like(total).index_add_(0, at, g.abs())
     return total, size, torch.bincount(at, minlength=rows).double()[:, None]
@@ -97,6 +101,7 @@ def test_types_and_widths(kind, out_kind, dim, B, gap, lead):
     (8200, 1201, 4096),                      # tiles of 16 in 16-bit types by the number of pieces
     (32_768, 5003, 24), (32_769, 5003, 8), (32_769, 5003, 24), (40_001, 5003, 63),    # groups of lanes from 32,769 on
     (65_535, 5003, 65), (65_536, 5003, 65), (70_001, 5003, 130), (66_000, 907, 500),  # tiles of 16 by the number of ids
+    (2_200_003, 50_021, 4),                  # more tiles than the blocks of a launch look at once
 ])
 def test_sizes(kind, out_kind, B, rows, dim):
     _both(rows, dim, B, kind, out_kind, seed=3)
@@ -211,3 +216,16 @@ def test_streams_and_graph(B, rows, dim):
         torch.cuda.synchronize()
         sums = emb.backward(ids, grad)
         assert torch.equal(into, emb.backward(ids, grad, out=sums, add=True))
+
+
+def test_a_table_without_rows():
+    """Every id is outside it."""
+    import torch
+    import paper_2206_10581_amd as tt
+    for B in (0, 5, 2000):
+        emb = tt.DenseEmbedding(torch.empty(0, 24, device="cuda"), 2000)
+        ids = torch.arange(B, device="cuda") - 2
+        grad = torch.ones(B, 24, device="cuda")
+        out = torch.full((B, 24), float("nan"), device="cuda")
+        assert not emb.forward(ids, out=out).any() and emb.backward(ids, grad).shape == (0, 24)
+        emb.backward_update(ids, grad, 1.0)
