@@ -11,8 +11,10 @@
  *                    phases of the timing breakdown; the paper prints no formula and names no
  *                    optimiser, so this is the chain rule through the two products and plain SGD)
  * and, for what is trained beside such a table, lookups and gradients of plain tables
- * (tt_emb_dense_forward, tt_emb_dense_backward) and the norm and clipping of a step's gradients
- * (tt_emb_grad_norm, tt_emb_grad_clip), which need no handle.
+ * (tt_emb_dense_forward, tt_emb_dense_backward), the norm and clipping of a step's gradients
+ * (tt_emb_grad_norm, tt_emb_grad_clip), log probabilities with their gradient (tt_emb_token_scores,
+ * tt_emb_token_backward, tt_emb_token_loss) and position biases of attention with theirs (tt_emb_bias_forward,
+ * tt_emb_bias_backward), none of which needs a handle.
  *
  * Naming.  The table has N = n1*n2*n3 rows (paper: M = m1 m2 m3) of D = d1*d2*d3 floats
  * (paper: N = n1 n2 n3); the TT ranks are (1, r1, r2, 1) (paper: R_0..R_3 with R_0 = R_3 = 1).
@@ -263,7 +265,7 @@ typedef struct {
   void* data;
   int64_t rows;
   int64_t ld;   /* values from the start of one row to the next, at least cols                     */
-  int32_t cols; /* 1 .. 65536                                                                       */
+  int32_t cols; /* 1 .. 65536 (logits: 1 .. 2^30)                                                     */
   int32_t type; /* TT_EMB_FP32, TT_EMB_BF16 or TT_EMB_FP16                                          */
 } tt_emb_matrix;
 
@@ -328,6 +330,109 @@ int tt_emb_grad_norm(const tt_emb_values* in, int32_t n, float scale, float* nor
  */
 int tt_emb_grad_clip(const tt_emb_values* in, const tt_emb_values* out, int32_t n, float scale, float max_norm,
                      float eps, float* norm, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* ---- the answers of a model: log probabilities of tokens (words, classes of nodes), and their gradient ---- */
+
+/*
+ * What tt_emb_token_scores writes for the n = logits->rows rows, device memory; a null pointer: not wanted.  At least
+ * one of the first five is.
+ */
+typedef struct {
+  float* logprob;     /* [n]       log probability of the row's token; needs tokens                  */
+  float* entropy;     /* [n]       -sum p log p                                                      */
+  float* state;       /* [2][n]    largest logit, and log of the sum of exp(scale * (logit - it)): what
+                                   tt_emb_token_backward needs                                       */
+  int64_t* top_ids;   /* [n][top]  the top likeliest tokens, the likeliest first, the lowest first among equals */
+  float* top_logprob; /* [n][top]  and their log probabilities; null together with top_ids           */
+  int32_t top;        /* 1 .. 64 (ignored without top_ids)                                            */
+  int32_t unused;
+} tt_emb_token_out;
+
+/* Bytes of workspace that tt_emb_token_scores and tt_emb_token_loss need, the same for all sizes. */
+int tt_emb_token_workspace_bytes(size_t* bytes);
+
+/*
+ * Scores of a row of logits x, for p_v = exp(scale * x_v) / sum_w exp(scale * x_w):  log p of the row's token, the entropy, and
+ * the likeliest tokens.  logits: rows below 2^30 and 1 .. 2^30 columns (a vocabulary, classes).  tokens: device
+ * int64[rows]; a row whose token is outside [0, cols) is left out: it is not read, and has log probability
+ * and entropy 0 and no likely tokens (id -1, log probability -infinity, as in the places behind the last column).  tokens null:
+ * all rows count.  scale > 0, finite (1 / temperature).  Sums are held in fp32 relative to the row's largest logit, in an order
+ * that the sizes alone fix; any logit may be -infinity (probability 0).  A row of -infinity alone has log probability -infinity,
+ * entropy 0 and no gradient; one with NaN or +infinity has NaN (and among the likeliest NaN comes before +infinity).
+ * workspace: device, 256-byte aligned; calls that share one must be ordered by a stream.  May be captured
+ * into a HIP graph.
+ */
+int tt_emb_token_scores(const tt_emb_matrix* logits, const int64_t* tokens, float scale, const tt_emb_token_out* out,
+                        void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Gradient of those with respect to the logits, for gradients d_logprob and d_entropy (device fp32[rows], at least one) of the
+ * log probabilities and the entropies:
+ *   dlogits[b,v] = scale * (d_logprob[b] * ((v = tokens[b]) - p_v) - d_entropy[b] * p_v * (log p_v + entropy[b]))
+ * with state and entropy (needed with d_entropy) as tt_emb_token_scores wrote them for these logits, tokens and scale.  Rows that
+ * are left out get zeros.  tokens may be null if d_logprob is.  dlogits: same rows and cols, any type, rounded once; it
+ * may be the logits themselves (same address, type and ld) and overlaps them no other way.
+ */
+int tt_emb_token_backward(const tt_emb_matrix* logits, const int64_t* tokens, float scale, const float* state,
+                          const float* entropy, const float* d_logprob, const float* d_entropy,
+                          const tt_emb_matrix* dlogits, void* hip_stream);
+
+/*
+ * Both for a loss that is known beforehand, -sum_b w_b * logprob[b]: writes logprob (device fp32[rows]) and the
+ * loss's gradient with respect to the logits.  w_b = weight * weights[b] (device fp32[rows], null: 1), weight finite.  dlogits and
+ * workspace as above.
+ */
+int tt_emb_token_loss(const tt_emb_matrix* logits, const int64_t* tokens, float scale, const float* weights, float weight,
+                      float* logprob, const tt_emb_matrix* dlogits, void* workspace, size_t workspace_bytes,
+                      void* hip_stream);
+
+/* ---- position bias of attention: a table looked up by distance ---- */
+
+/* A value for every head and pair of a query and a key, device memory: (b, h, i, j) at
+ * data + b * batch_ld + h * head_ld + i * query_ld + j.  Read only, strides may be 0 (the same values again). */
+typedef struct {
+  void* data;
+  int64_t batch_ld, head_ld, query_ld; /* 0 .. 2^40                                                    */
+  int64_t queries, keys;               /* 0 .. 2^30 - 1                                                */
+  int32_t batch, heads;                /* 0 .. 2^30 - 1; batch * heads * queries * keys below 2^50      */
+  int32_t type;                        /* TT_EMB_FP32, TT_EMB_BF16 or TT_EMB_FP16                      */
+  int32_t unused;
+} tt_emb_pairs;
+
+/* The distance of key j from query i in sequence b is j - i + offset + offsets[b], and its bucket
+ * bucket_of[span + distance], for distances beyond -span and span that of these.  A bucket outside the table: none. */
+typedef struct {
+  const int32_t* bucket_of; /* device int32[2 * span + 1]                                               */
+  const int64_t* offsets;   /* device int64[batch], or null: 0                                          */
+  int64_t offset;           /* the first key's position less the first query's; sums with offsets are taken
+                               as if cut at -2^40 and 2^40, beyond all distances                        */
+  int32_t span;             /* 0 .. 2^20                                                                */
+  int32_t unused;
+} tt_emb_distances;
+
+/*
+ * out[b,h,i,j] = in[b,h,i,j] + table[bucket,h] for the bucket of (b,i,j), or without `in` the second term alone; where there is no
+ * bucket, `fill` (-infinity: a mask) stands for the table's value.  An infinite value of table or fill replaces in's,
+ * whatever that holds.  table: [buckets][heads], heads up to 65536.  in: sizes as out; may be out itself (same address, type and
+ * strides) and overlaps it no other way.  Any types; sums in fp32, rounded once.  May be captured into a HIP graph.
+ */
+int tt_emb_bias_forward(const tt_emb_matrix* table, const tt_emb_distances* distances, float fill,
+                        const tt_emb_pairs* in, const tt_emb_pairs* out, void* hip_stream);
+
+/* Bytes of workspace that tt_emb_bias_backward needs for gradients of these sizes (strides, type and data do not matter),
+ * with or without offsets for each sequence. */
+int tt_emb_bias_workspace_bytes(const tt_emb_pairs* grad, int32_t span, size_t* bytes);
+
+/*
+ * Gradient of that with respect to the table:
+ *   sum[u,h] = sum of grad[b,h,i,j] over all places (b,i,j) of bucket u
+ *   add = 0   dtable = sum;   add = 1   dtable = dtable + sum
+ * Places without a bucket are not read into any sum.  Sums are formed in fp32 over a few hundred places and in fp64 beyond, in a
+ * fixed order, and rounded once.  workspace: device, 256-byte aligned; calls that share one must be ordered by a
+ * stream.  May be captured into a HIP graph.
+ */
+int tt_emb_bias_backward(const tt_emb_pairs* grad, const tt_emb_distances* distances, const tt_emb_matrix* dtable, int add,
+                         void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /*
  * Per-kernel timing for benchmarks.  While enabled, every kernel launch is bracketed by a pair of

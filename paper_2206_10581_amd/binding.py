@@ -5,10 +5,12 @@ There is no fallback: if the shared library has not been built, loading raises.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 import warnings
 from ctypes import POINTER, byref, c_char_p, c_double, c_float, c_int, c_int32, c_int64, c_size_t, \
     c_uint32, c_void_p
+from typing import Any, NamedTuple
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libtt_emb.so")
@@ -36,6 +38,21 @@ class TTEmbMatrix(ctypes.Structure):
 
 class TTEmbValues(ctypes.Structure):
     _fields_ = [("data", c_void_p), ("count", c_int64), ("type", c_int32), ("unused", c_int32)]
+
+
+class TTEmbTokenOut(ctypes.Structure):
+    _fields_ = [("logprob", c_void_p), ("entropy", c_void_p), ("state", c_void_p), ("top_ids", c_void_p),
+                ("top_logprob", c_void_p), ("top", c_int32), ("unused", c_int32)]
+
+
+class TTEmbPairs(ctypes.Structure):
+    _fields_ = [("data", c_void_p), ("batch_ld", c_int64), ("head_ld", c_int64), ("query_ld", c_int64),
+                ("queries", c_int64), ("keys", c_int64), ("batch", c_int32), ("heads", c_int32), ("type", c_int32),
+                ("unused", c_int32)]
+
+
+class TTEmbDistances(ctypes.Structure):
+    _fields_ = [("bucket_of", c_void_p), ("offsets", c_void_p), ("offset", c_int64), ("span", c_int32), ("unused", c_int32)]
 
 
 class TTEmbError(RuntimeError):
@@ -84,6 +101,15 @@ def load_library():
     lib.tt_emb_grad_norm.argtypes = [valp, c_int32, c_float, c_void_p, c_void_p, c_size_t, c_void_p]
     lib.tt_emb_grad_clip.argtypes = [valp, valp, c_int32, c_float, c_float, c_float, c_void_p, c_void_p, c_size_t,
                                      c_void_p]
+    tokp, pairp, distp = POINTER(TTEmbTokenOut), POINTER(TTEmbPairs), POINTER(TTEmbDistances)
+    lib.tt_emb_token_workspace_bytes.argtypes = [POINTER(c_size_t)]
+    lib.tt_emb_token_scores.argtypes = [matp, c_void_p, c_float, tokp, c_void_p, c_size_t, c_void_p]
+    lib.tt_emb_token_backward.argtypes = [matp, c_void_p, c_float, c_void_p, c_void_p, c_void_p, c_void_p, matp, c_void_p]
+    lib.tt_emb_token_loss.argtypes = [matp, c_void_p, c_float, c_void_p, c_float, c_void_p, matp, c_void_p, c_size_t,
+                                      c_void_p]
+    lib.tt_emb_bias_forward.argtypes = [matp, distp, c_float, pairp, pairp, c_void_p]
+    lib.tt_emb_bias_workspace_bytes.argtypes = [pairp, c_int32, POINTER(c_size_t)]
+    lib.tt_emb_bias_backward.argtypes = [pairp, distp, matp, c_int, c_void_p, c_size_t, c_void_p]
     lib.tt_emb_profile_enable.argtypes = [c_void_p, c_int]
     lib.tt_emb_profile_slots.argtypes = []
     lib.tt_emb_profile_read.argtypes = [c_void_p, c_int, POINTER(c_char_p), POINTER(c_int64),
@@ -98,6 +124,8 @@ def load_library():
                  "tt_emb_set_reindex", "tt_emb_set_adagrad", "tt_emb_set_adam", "tt_emb_wait_backward", "tt_emb_get_stats", "tt_emb_profile_enable",
                  "tt_emb_dense_forward", "tt_emb_dense_workspace_bytes", "tt_emb_dense_backward",
                  "tt_emb_norm_workspace_bytes", "tt_emb_grad_norm", "tt_emb_grad_clip",
+                 "tt_emb_token_workspace_bytes", "tt_emb_token_scores", "tt_emb_token_backward", "tt_emb_token_loss",
+                 "tt_emb_bias_forward", "tt_emb_bias_workspace_bytes", "tt_emb_bias_backward",
                  "tt_emb_profile_slots", "tt_emb_profile_read", "tt_emb_profile_peaks", "tt_emb_destroy"):
         getattr(lib, name).restype = c_int
     _lib = lib
@@ -243,6 +271,51 @@ def tt_emb_grad_norm(values, n: int, scale: float, norm_ptr: int, ws_ptr: int, w
 def tt_emb_grad_clip(values, out, n: int, scale: float, max_norm: float, eps: float, norm_ptr: int, ws_ptr: int,
                      ws_bytes: int, stream: int) -> int:
     return load_library().tt_emb_grad_clip(values, out, n, scale, max_norm, eps, norm_ptr, ws_ptr, ws_bytes, stream)
+
+
+def _ref(structure):
+    return None if structure is None else byref(structure)
+
+
+def tt_emb_token_workspace_bytes():
+    out = c_size_t(0)
+    rc = load_library().tt_emb_token_workspace_bytes(byref(out))
+    return rc, int(out.value)
+
+
+def tt_emb_token_scores(logits: TTEmbMatrix, tokens_ptr: int, scale: float, out: TTEmbTokenOut, ws_ptr: int, ws_bytes: int,
+                        stream: int) -> int:
+    return load_library().tt_emb_token_scores(_ref(logits), tokens_ptr, scale, _ref(out), ws_ptr, ws_bytes, stream)
+
+
+def tt_emb_token_backward(logits: TTEmbMatrix, tokens_ptr: int, scale: float, state_ptr: int, entropy_ptr: int,
+                          d_logprob_ptr: int, d_entropy_ptr: int, dlogits: TTEmbMatrix, stream: int) -> int:
+    return load_library().tt_emb_token_backward(_ref(logits), tokens_ptr, scale, state_ptr, entropy_ptr, d_logprob_ptr,
+                                                d_entropy_ptr, _ref(dlogits), stream)
+
+
+def tt_emb_token_loss(logits: TTEmbMatrix, tokens_ptr: int, scale: float, weights_ptr: int, weight: float,
+                      logprob_ptr: int, dlogits: TTEmbMatrix, ws_ptr: int, ws_bytes: int, stream: int) -> int:
+    return load_library().tt_emb_token_loss(_ref(logits), tokens_ptr, scale, weights_ptr, weight, logprob_ptr,
+                                            _ref(dlogits), ws_ptr, ws_bytes, stream)
+
+
+def tt_emb_bias_forward(table: TTEmbMatrix, distances: TTEmbDistances, fill: float, scores, out: TTEmbPairs,
+                        stream: int) -> int:
+    """scores: a TTEmbPairs, or None for the bias alone."""
+    return load_library().tt_emb_bias_forward(_ref(table), _ref(distances), fill, _ref(scores), _ref(out), stream)
+
+
+def tt_emb_bias_workspace_bytes(grad: TTEmbPairs, span: int):
+    out = c_size_t(0)
+    rc = load_library().tt_emb_bias_workspace_bytes(_ref(grad), span, byref(out))
+    return rc, int(out.value)
+
+
+def tt_emb_bias_backward(grad: TTEmbPairs, distances: TTEmbDistances, dtable: TTEmbMatrix, add: bool, ws_ptr: int,
+                         ws_bytes: int, stream: int) -> int:
+    return load_library().tt_emb_bias_backward(_ref(grad), _ref(distances), _ref(dtable), 1 if add else 0, ws_ptr, ws_bytes,
+                                               stream)
 
 
 # ---- convenience wrappers over torch tensors (memory and streams only)
@@ -463,6 +536,15 @@ class _OnDevice:
             return TT_EMB_FP16
         raise ValueError(f"type {kind}: float32, bfloat16 or float16 needed")
 
+    def _matrix(self, t):
+        if t.dim() != 2 or t.device != self.device:
+            raise ValueError(f"matrix on {self.device} needed: shape {tuple(t.shape)} on {t.device}")
+        rows, cols = t.shape
+        step, side = t.stride()
+        if cols > 1 and side != 1 or rows > 1 and step < cols:
+            raise ValueError(f"strides {t.stride()}: values of a row side by side, rows that do not overlap needed")
+        return TTEmbMatrix(t.data_ptr(), rows, step if rows > 1 else cols, cols, self._type(t))
+
     def _make_workspace(self, nbytes):
         self._home = self._stream(self.index)  # the workspace belongs to this stream
         self.workspace = self.torch.empty(nbytes + 256, dtype=self.torch.uint8, device=self.device)
@@ -484,15 +566,6 @@ class DenseEmbedding(_OnDevice):
         self.padding_id = -1 if padding_id is None else int(padding_id)
         self._described, self._table, self._spaces, self.workspace_bytes = None, None, [], 0
         self._weight()
-
-    def _matrix(self, t):
-        if t.dim() != 2 or t.device != self.device:
-            raise ValueError(f"matrix on {self.device} needed: shape {tuple(t.shape)} on {t.device}")
-        rows, cols = t.shape
-        step, side = t.stride()
-        if cols > 1 and side != 1 or rows > 1 and step < cols:
-            raise ValueError(f"strides {t.stride()}: values of a row side by side, rows that do not overlap needed")
-        return TTEmbMatrix(t.data_ptr(), rows, step if rows > 1 else cols, cols, self._type(t))
 
     def _ids(self, ids):
         if ids.dtype != self.torch.int64 or ids.device != self.device or ids.dim() != 1 or not ids.is_contiguous():
@@ -686,4 +759,239 @@ class GradientClip(_OnDevice):
         out = self._norm(out)
         self._call(self.lib.tt_emb_grad_clip, self._in, self._out, len(self._in), float(scale), float(max_norm), float(eps),
                    out.data_ptr(), self._ws_ptr, self.workspace_bytes)
+        return out
+
+
+class TokenResult(NamedTuple):
+    """What TokenScores.forward returns; None: not asked for."""
+    logprobs: Any = None      # [n] log probabilities of the tokens
+    entropy: Any = None       # [n]
+    top_ids: Any = None       # [n, top] the likeliest tokens, int64; -1: none
+    top_logprobs: Any = None  # [n, top]
+    state: Any = None         # for backward
+
+
+class TokenScores(_OnDevice):
+    """Scores of rows of logits [n, columns] (a vocabulary, classes): log probability of a token for each row, entropy, the
+    likeliest tokens; and the logits' gradient.
+
+    p = softmax(scale * logits); scale: 1 / temperature.  Logits: float32, bfloat16 or float16, values of a row side by side.
+    tokens: int64, one a row; a row whose token is no column (-1, -100, ...) is left out: its logits are not read, its log
+    probability, entropy and gradient are 0.  Logits of -infinity have probability 0; a row of them alone has log probability
+    -infinity, entropy 0 and no gradient; NaN and +infinity make a row's numbers NaN.  Must not be used from two
+    threads or streams at once (the workspace)."""
+
+    def __init__(self, scale: float = 1.0, device="cuda:0"):
+        import torch
+        device = torch.device(device)
+        if device.type == "cuda" and device.index is None:
+            device = torch.device("cuda", torch.cuda.current_device())
+        super().__init__(device)
+        self.scale = float(scale)
+        if not 0.0 < self.scale < math.inf:
+            raise ValueError(f"scale {scale}: positive and finite needed")
+        rc, nbytes = tt_emb_token_workspace_bytes()
+        if rc:
+            raise TTEmbError(rc, "tt_emb_token_workspace_bytes")
+        self._make_workspace(nbytes)
+
+    def _vector(self, t, n, kind, name):
+        if t.dtype != kind or t.device != self.device or t.shape != (n,) or not t.is_contiguous():
+            raise ValueError(f"{name}: contiguous {kind} [{n}] on {self.device} needed, not {t.dtype} {tuple(t.shape)} on "
+                             f"{t.device}")
+        return t.data_ptr()
+
+    def _empty(self, *shape, dtype=None):
+        return self.torch.empty(shape, dtype=dtype or self.torch.float32, device=self.device)
+
+    def _out(self, logits, out, dtype):
+        if out is None:
+            return self.torch.empty(logits.shape, dtype=dtype or logits.dtype, device=self.device)
+        if out.shape != logits.shape or dtype not in (None, out.dtype):
+            raise ValueError(f"out: {tuple(logits.shape)} of {dtype or out.dtype} needed, not {tuple(out.shape)}")
+        return out
+
+    def forward(self, logits, tokens=None, entropy: bool = False, top: int = 0, state: bool = False):
+        """A TokenResult: log probabilities of tokens (without tokens all rows count and there are none), entropies, the
+        `top` (up to 64) likeliest tokens, the lowest first among equals, and what backward needs."""
+        x = self._matrix(logits)
+        n, torch = x.rows, self.torch
+        ptr = 0 if tokens is None else self._vector(tokens, n, torch.int64, "tokens")
+        if not 0 <= top <= 64:
+            raise ValueError(f"top {top}: 0 to 64 needed")
+        if tokens is None and not (entropy or top or state):
+            raise ValueError("tokens, entropy, top or state needed")
+        logprobs = None if tokens is None else self._empty(n)
+        h = self._empty(n) if entropy else None
+        kept = self._empty(2, n) if state else None
+        ids, values = (self._empty(n, top, dtype=torch.int64), self._empty(n, top)) if top else (None, None)
+        at = [0 if t is None else t.data_ptr() for t in (logprobs, h, kept, ids, values)]
+        self._call(self.lib.tt_emb_token_scores, byref(x), ptr, self.scale, byref(TTEmbTokenOut(*at, top, 0)), self._ws_ptr,
+                   self.workspace_bytes)
+        return TokenResult(logprobs, h, ids, values, (kept, h) if state else None)
+
+    def backward(self, logits, tokens, state, d_logprobs=None, d_entropy=None, out=None, dtype=None):
+        """Gradient of a forward(..., state=True) of the same logits and tokens with respect to the logits, for
+        gradients of the log probabilities and (with entropy=True there) of the entropies, float32 [n].  out: may be the
+        logits themselves, which are overwritten."""
+        x = self._matrix(logits)
+        n, torch = x.rows, self.torch
+        if d_logprobs is None and d_entropy is None:
+            raise ValueError("d_logprobs or d_entropy needed")
+        if tokens is None and d_logprobs is not None:
+            raise ValueError("d_logprobs needs tokens")
+        kept, h = state
+        if kept.shape != (2, n) or not kept.is_contiguous() or kept.dtype != torch.float32 or kept.device != self.device:
+            raise ValueError(f"state of {n} rows on {self.device} needed")
+        if d_entropy is not None and h is None:
+            raise ValueError("d_entropy needs the state of a forward with entropy=True")
+        at = [0 if d is None else self._vector(d, n, torch.float32, name) for d, name in
+              ((h if d_entropy is not None else None, "entropy"), (d_logprobs, "d_logprobs"), (d_entropy, "d_entropy"))]
+        ptr = 0 if tokens is None else self._vector(tokens, n, torch.int64, "tokens")
+        out = self._out(logits, out, dtype)
+        self._call(self.lib.tt_emb_token_backward, byref(x), ptr, self.scale, kept.data_ptr(), *at,
+                   byref(self._matrix(out)))
+        return out
+
+    def loss(self, logits, tokens, weights=1.0, out=None, dtype=None):
+        """Log probabilities of the tokens, and the gradient of the loss -sum(weights * log probabilities) with respect to the
+        logits, in one call.  weights: a number, or float32 [n].  out: as in backward."""
+        x = self._matrix(logits)
+        n, torch = x.rows, self.torch
+        ptr = self._vector(tokens, n, torch.int64, "tokens")
+        each, one = (self._vector(weights, n, torch.float32, "weights"), 1.0) if isinstance(weights, torch.Tensor) else (
+            0, float(weights))
+        out, logprobs = self._out(logits, out, dtype), self._empty(n)
+        self._call(self.lib.tt_emb_token_loss, byref(x), ptr, self.scale, each, one, logprobs.data_ptr(),
+                   byref(self._matrix(out)), self._ws_ptr, self.workspace_bytes)
+        return logprobs, out
+
+
+class PositionBias(_OnDevice):
+    """A learned bias of attention by distance: table [buckets, heads], looked up by the bucket of every distance of a key
+    from a query, alone or added to scores [batch, heads, queries, keys]; and the table's gradient.
+
+    The distance of key j from query i is j - i + offset, offset: the first key's position less the first query's, a
+    number, or int64 [batch] with one for each sequence.  (A query that follows a cache of n keys, its own among them: 1 - n.)
+    bucket_of: int32 [2 * span + 1], the buckets of the distances -span to span, whose ends also stand for all beyond; a
+    number outside the table: no bucket, where `fill` (-inf: a mask) stands for the bias.  An infinite bias replaces the score
+    that it would be added to, whatever that is.  weight (float32, bfloat16 or float16, values of a row side by side) and bucket_of
+    are borrowed, and taken as they are at the time of a call.  Must not be used from two threads or streams
+    at once (the workspace of backward)."""
+
+    def __init__(self, weight, bucket_of, fill: float = 0.0):
+        super().__init__(weight.device)
+        self.weight, self.bucket_of, self.fill = weight, bucket_of, float(fill)
+        if self.fill != self.fill:
+            raise ValueError("fill: a number needed")
+        self._spaces, self.workspace_bytes = [], 0
+        self._make_workspace(256)
+        self._matrix(weight)
+        self._distances(0, 1)
+
+    @staticmethod
+    def log_buckets(buckets: int, max_distance: int, bidirectional: bool = True):
+        """bucket_of (on the CPU) for buckets that widen with the distance: half of a side's buckets hold one distance each,
+        from 0 on; the others grow by a constant factor up to max_distance, and the last holds all beyond.  Bucket e + k starts at
+        the smallest whole number that is at least e (max_distance / e) ** (k / (side - e)), e the first half's size.
+        bidirectional: the first half of the buckets is for keys at and before a query, the second for keys after it; else
+        keys after a query have no bucket (-1)."""
+        import torch
+        side = buckets // 2 if bidirectional else buckets
+        near = side // 2
+        if near < 1 or bidirectional and buckets % 2 or max_distance <= near:
+            raise ValueError(f"{buckets} buckets up to distance {max_distance}: at least two a side, an even number for "
+                             "both sides, and a distance beyond the first half needed")
+        far, starts = side - near, []
+        for k in range(1, far):
+            # the smallest n with n ** far >= near ** (far - k) * max_distance ** k, in whole numbers
+            power = near ** (far - k) * max_distance ** k
+            low, high = near, max_distance
+            while low < high:
+                middle = (low + high) // 2
+                low, high = (low, middle) if middle ** far >= power else (middle + 1, high)
+            starts.append(low)
+        distance = torch.arange(max_distance + 1)
+        before = torch.where(distance < near, distance, near + torch.bucketize(distance, torch.tensor(starts, dtype=torch.int64),
+                                                                               right=True))
+        after = side + before[1:] if bidirectional else torch.full((max_distance,), -1)
+        return torch.cat([before.flip(0), after]).to(torch.int32)
+
+    def _distances(self, offset, batch):
+        of, torch = self.bucket_of, self.torch
+        if of.dtype != torch.int32 or of.device != self.device or of.dim() != 1 or not of.is_contiguous() or of.numel() % 2 == 0:
+            raise ValueError(f"bucket_of: contiguous int32 [2 * span + 1] on {self.device} needed")
+        at, number = 0, 0
+        if isinstance(offset, torch.Tensor):
+            if offset.dtype != torch.int64 or offset.device != self.device or offset.shape != (batch,) or \
+                    not offset.is_contiguous():
+                raise ValueError(f"offset: a number, or contiguous int64 [{batch}] on {self.device} needed")
+            at = offset.data_ptr()
+        else:
+            number = max(-(1 << 60), min(1 << 60, int(offset)))  # far beyond all distances
+        return TTEmbDistances(of.data_ptr(), at, number, of.numel() // 2, 0)
+
+    def _pairs(self, t, written=False):
+        if t.dim() != 4 or t.device != self.device:
+            raise ValueError(f"[batch, heads, queries, keys] on {self.device} needed: shape {tuple(t.shape)} on {t.device}")
+        b, h, q, k = t.shape
+        steps = t.stride()
+        if k > 1 and steps[3] != 1:
+            raise ValueError(f"strides {steps}: keys side by side needed")
+        if h != self.weight.shape[1]:
+            raise ValueError(f"{h} heads, not the table's {self.weight.shape[1]}")
+        if written and t.numel():
+            size = 1
+            for step, n in sorted((s, n) for s, n in zip(steps, t.shape) if n > 1):
+                if step < size:
+                    raise ValueError(f"strides {steps}: values that do not overlap needed")
+                size = step * (n - 1) + size
+        return TTEmbPairs(t.data_ptr(), steps[0] if b > 1 else 0, steps[1] if h > 1 else 0, steps[2] if q > 1 else 0, q, k, b, h,
+                          self._type(t), 0)
+
+    def forward(self, queries: int, keys: int, offset=0, out=None, dtype=None):
+        """The bias, [batch, heads, queries, keys], in the table's type unless out or dtype says otherwise.  batch: that of out or
+        of the offsets, or 1."""
+        torch, table = self.torch, self._matrix(self.weight)
+        if out is None:
+            batch = offset.numel() if isinstance(offset, torch.Tensor) else 1
+            out = torch.empty((batch, table.cols, queries, keys), dtype=dtype or self.weight.dtype, device=self.device)
+        elif out.shape[2:] != (queries, keys) or dtype not in (None, out.dtype):
+            raise ValueError(f"out: [batch, heads, {queries}, {keys}] of {dtype or out.dtype} needed, not {tuple(out.shape)}")
+        to = self._pairs(out, True)
+        self._call(self.lib.tt_emb_bias_forward, byref(table), byref(self._distances(offset, to.batch)), self.fill, None,
+                   byref(to))
+        return out
+
+    def add_to(self, scores, offset=0, out=None):
+        """scores + bias, in out, or (None) in place."""
+        if out is None:
+            out = scores
+        elif out.shape != scores.shape:
+            raise ValueError(f"out: {tuple(scores.shape)} needed, not {tuple(out.shape)}")
+        table, to = self._matrix(self.weight), self._pairs(out, True)
+        given = to if out is scores else self._pairs(scores)
+        self._call(self.lib.tt_emb_bias_forward, byref(table), byref(self._distances(offset, to.batch)), self.fill,
+                   byref(given), byref(to))
+        return out
+
+    def backward(self, grad, offset=0, out=None, dtype=None, add: bool = False):
+        """Gradient with respect to the table, [buckets, heads], for the gradient of the bias or of the scores that it was added
+        to.  With add, it is added to out."""
+        g, weight = self._pairs(grad), self.weight
+        if out is None:
+            if add:
+                raise ValueError("add needs out")
+            out = self.torch.empty(weight.shape, dtype=dtype or weight.dtype, device=self.device)
+        elif out.shape != weight.shape or dtype not in (None, out.dtype):
+            raise ValueError(f"out: {tuple(weight.shape)} of {dtype or out.dtype} needed, not {tuple(out.shape)}")
+        d = self._distances(offset, g.batch)
+        rc, nbytes = tt_emb_bias_workspace_bytes(g, d.span)
+        if rc:
+            raise TTEmbError(rc, "tt_emb_bias_workspace_bytes")
+        if nbytes > self.workspace_bytes:
+            self._make_workspace(nbytes)
+            self._spaces.append(self.workspace)  # a captured graph may go on using a smaller one
+        self._call(self.lib.tt_emb_bias_backward, byref(g), byref(d), byref(self._matrix(out)), 1 if add else 0, self._ws_ptr,
+                   self.workspace_bytes)
         return out

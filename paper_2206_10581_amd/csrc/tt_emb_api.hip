@@ -93,6 +93,17 @@ int64_t clip_units(int64_t count);
 void launch_put_items(const PutList&, int n, int64_t first, ClipItem* to, hipStream_t);
 void launch_norm(const ClipTensors&, double* parts, float scale, float* norm, hipStream_t);
 void launch_clip(const ClipTensors&, double* parts, float scale, float max_norm, float eps, float* norm, hipStream_t);
+// scores of logits (tt_emb_tokens.hip) and position bias (tt_emb_bias.hip)
+void launch_token_scores(const TokenRows&, int type, const TokenOut&, const TokenParts&, hipStream_t);
+void launch_token_grad(const TokenRows&, int type, const float* state, const float* entropy, const float* d_logprob,
+                       const float* d_entropy, const tt_emb_matrix& dx, hipStream_t);
+void launch_token_loss(const TokenRows&, int type, const float* weights, float weight, float* logprob,
+                       const tt_emb_matrix& dx, hipStream_t);
+void launch_bias(const tt_emb_matrix& table, const tt_emb_distances&, float fill, const tt_emb_pairs* in,
+                 const tt_emb_pairs& out, hipStream_t);
+SumPlan sum_plan(const tt_emb_pairs&, int span, bool offsets);
+void launch_bias_sums(const tt_emb_pairs&, const tt_emb_distances&, const tt_emb_matrix& out, bool add, float* parts,
+                      hipStream_t);
 hipError_t calibrate(void* buf, size_t bytes, hipStream_t, double* copy_bytes_per_s,
                      double* mfma_flops_per_s, double* gather_bytes_per_s,
                      double* far_gather_bytes_per_s);
@@ -981,16 +992,65 @@ static int backward_indexed(tt_emb* h, const float* grad_out, float lr, int B, h
 // ---- plain tables, norm and clipping ----
 
 static bool known_type(int type) { return type == TT_EMB_FP32 || type == TT_EMB_BF16 || type == TT_EMB_FP16; }
-static size_t type_bytes(int type) { return type == TT_EMB_FP32 ? 4 : 2; }
+static size_t type_bytes(int type) { return (size_t)type_size(type); }
 constexpr int kDenseCols = 1 << 16;  // widest row
 constexpr int64_t kDenseBatch = int64_t(1) << 30;
 
-static bool good_matrix(const tt_emb_matrix* m, int64_t most_rows) {
+static bool good_matrix(const tt_emb_matrix* m, int64_t most_rows, int most_cols = kDenseCols) {
   return m != nullptr && known_type(m->type) && m->rows >= 0 && m->rows < most_rows && m->cols >= 1 &&
-         m->cols <= kDenseCols && m->ld >= m->cols && m->ld <= (int64_t(1) << 40) &&
+         m->cols <= most_cols && m->ld >= m->cols && m->ld <= (int64_t(1) << 40) &&
          (m->rows == 0 || m->data != nullptr) && ((uintptr_t)m->data & (type_bytes(m->type) - 1)) == 0;
 }
 static bool good_ids(const int64_t* ids, int64_t B) { return B == 0 || (ids != nullptr && ((uintptr_t)ids & 7u) == 0); }
+
+// ---- scores of logits, position bias ----
+
+constexpr int kTokenCols = 1 << 30;
+constexpr size_t kTokenSums = sizeof(f4) * kTokenParts, kTokenBytes = kTokenSums + sizeof(uint64_t) * kWave * kTokenParts;
+
+static bool good_floats(const void* p) { return ((uintptr_t)p & 3u) == 0; }
+static bool good_logits(const tt_emb_matrix* m, const int64_t* tokens, float scale) {
+  return good_matrix(m, kDenseBatch, kTokenCols) && ((uintptr_t)tokens & 7u) == 0 && scale > 0.f && std::isfinite(scale);
+}
+static TokenRows token_rows(const tt_emb_matrix& m, const int64_t* tokens, float scale) {
+  return {m.data, m.ld, m.rows, m.cols, tokens, scale, (float)((double)scale * 1.4426950408889634)};
+}
+static int check_workspace(const void* workspace, size_t bytes, size_t needed) {
+  if (workspace == nullptr || ((uintptr_t)workspace & 255u) != 0) return TT_EMB_EINVAL;
+  return bytes < needed ? TT_EMB_ENOSPC : TT_EMB_OK;
+}
+// Whether two matrices of the same size are the same one, or share no byte.  Of two with different pitches the whole ranges
+// count.
+static bool same_or_apart(const tt_emb_matrix& a, const tt_emb_matrix& b) {
+  if (a.rows == 0 || (a.data == b.data && a.type == b.type && (a.ld == b.ld || a.rows == 1))) return true;
+  const int64_t sa = type_size(a.type), sb = type_size(b.type), pa = a.ld * sa, pb = b.ld * sb;
+  const int64_t wa = a.cols * sa, wb = b.cols * sb, at = (int64_t)((uintptr_t)b.data - (uintptr_t)a.data);
+  if (at >= (a.rows - 1) * pa + wa || -at >= (b.rows - 1) * pb + wb) return true;
+  if (pa != pb || a.rows == 1) return false;
+  const int64_t in = (at % pa + pa) % pa;  // where b's rows start in a's
+  return in >= wa && in + wb <= pa;
+}
+// dx is as large as the logits, and apart from them or in their place.
+static bool good_gradient(const tt_emb_matrix* m, const tt_emb_matrix* dx) {
+  return good_matrix(dx, kDenseBatch, kTokenCols) && dx->rows == m->rows && dx->cols == m->cols && same_or_apart(*m, *dx);
+}
+
+constexpr int64_t kPairsMost = int64_t(1) << 30, kPairsStep = int64_t(1) << 40;
+static bool good_sizes(const tt_emb_pairs* p) {
+  if (p == nullptr || p->batch < 0 || p->heads < 0 || p->queries < 0 || p->keys < 0) return false;
+  if (p->batch >= kPairsMost || p->heads >= kPairsMost || p->queries >= kPairsMost || p->keys >= kPairsMost) return false;
+  return (double)p->batch * p->heads * (double)p->queries * (double)p->keys < 1125899906842624.0;
+}
+static bool no_pairs(const tt_emb_pairs& p) { return p.batch == 0 || p.heads == 0 || p.queries == 0 || p.keys == 0; }
+static bool good_pairs(const tt_emb_pairs* p) {
+  auto step = [](int64_t s) { return s >= 0 && s <= kPairsStep; };
+  return good_sizes(p) && known_type(p->type) && step(p->batch_ld) && step(p->head_ld) && step(p->query_ld) &&
+         (no_pairs(*p) || p->data != nullptr) && ((uintptr_t)p->data & (type_bytes(p->type) - 1)) == 0;
+}
+static bool good_distances(const tt_emb_distances* d) {
+  return d != nullptr && d->bucket_of != nullptr && ((uintptr_t)d->bucket_of & 3u) == 0 && ((uintptr_t)d->offsets & 7u) == 0 &&
+         d->span >= 0 && d->span <= 1 << 20;
+}
 
 static size_t carve_dense(int cols, int64_t max_batch, char* base, DenseWork* ws) {
   size_t off = 0;
@@ -1317,6 +1377,104 @@ int tt_emb_grad_clip(const tt_emb_values* in, const tt_emb_values* out, int32_t 
   ClipList list;
   const ClipTensors t = clip_tensors(in, out, n, &list, workspace, st);
   launch_clip(t, (double*)workspace, scale, max_norm, eps, norm, st);
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? TT_EMB_OK : hip_fail(e);
+}
+
+int tt_emb_token_workspace_bytes(size_t* bytes) {
+  if (bytes == nullptr) return TT_EMB_EINVAL;
+  *bytes = kTokenBytes;
+  return TT_EMB_OK;
+}
+
+int tt_emb_token_scores(const tt_emb_matrix* logits, const int64_t* tokens, float scale, const tt_emb_token_out* out,
+                        void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (!good_logits(logits, tokens, scale) || out == nullptr) return TT_EMB_EINVAL;
+  const bool list = out->top_ids != nullptr;
+  if (list != (out->top_logprob != nullptr) || (list && (out->top < 1 || out->top > kWave))) return TT_EMB_EINVAL;
+  if (((uintptr_t)out->top_ids & 7u) != 0 || !good_floats(out->top_logprob) || !good_floats(out->logprob) ||
+      !good_floats(out->entropy) || !good_floats(out->state))
+    return TT_EMB_EINVAL;
+  const int rc = check_workspace(workspace, workspace_bytes, kTokenBytes);
+  if (rc != TT_EMB_OK) return rc;
+  if (logits->rows == 0) return TT_EMB_OK;
+  if (out->logprob != nullptr && tokens == nullptr) return TT_EMB_EINVAL;
+  if (out->logprob == nullptr && out->entropy == nullptr && out->state == nullptr && !list) return TT_EMB_EINVAL;
+  const TokenOut o{out->logprob, out->entropy, out->state, out->top_ids, out->top_logprob, list ? out->top : 0};
+  const TokenParts parts{(f4*)workspace, (unsigned long long*)((char*)workspace + kTokenSums)};
+  launch_token_scores(token_rows(*logits, tokens, scale), logits->type, o, parts, (hipStream_t)hip_stream);
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? TT_EMB_OK : hip_fail(e);
+}
+
+int tt_emb_token_backward(const tt_emb_matrix* logits, const int64_t* tokens, float scale, const float* state,
+                          const float* entropy, const float* d_logprob, const float* d_entropy,
+                          const tt_emb_matrix* dlogits, void* hip_stream) {
+  if (!good_logits(logits, tokens, scale) || !good_gradient(logits, dlogits)) return TT_EMB_EINVAL;
+  if (!good_floats(state) || !good_floats(entropy) || !good_floats(d_logprob) || !good_floats(d_entropy)) return TT_EMB_EINVAL;
+  if (logits->rows == 0) return TT_EMB_OK;
+  if (state == nullptr || (d_logprob == nullptr && d_entropy == nullptr) || (d_logprob != nullptr && tokens == nullptr) ||
+      (d_entropy != nullptr && entropy == nullptr))
+    return TT_EMB_EINVAL;
+  launch_token_grad(token_rows(*logits, tokens, scale), logits->type, state, entropy, d_logprob, d_entropy, *dlogits,
+                    (hipStream_t)hip_stream);
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? TT_EMB_OK : hip_fail(e);
+}
+
+int tt_emb_token_loss(const tt_emb_matrix* logits, const int64_t* tokens, float scale, const float* weights, float weight,
+                      float* logprob, const tt_emb_matrix* dlogits, void* workspace, size_t workspace_bytes,
+                      void* hip_stream) {
+  if (!good_logits(logits, tokens, scale) || !good_gradient(logits, dlogits) || !good_floats(weights) ||
+      !good_floats(logprob) || !std::isfinite(weight))
+    return TT_EMB_EINVAL;
+  const int rc = check_workspace(workspace, workspace_bytes, kTokenBytes);
+  if (rc != TT_EMB_OK) return rc;
+  if (logits->rows == 0) return TT_EMB_OK;
+  if (tokens == nullptr || logprob == nullptr) return TT_EMB_EINVAL;
+  launch_token_loss(token_rows(*logits, tokens, scale), logits->type, weights, weight, logprob, *dlogits,
+                    (hipStream_t)hip_stream);
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? TT_EMB_OK : hip_fail(e);
+}
+
+int tt_emb_bias_forward(const tt_emb_matrix* table, const tt_emb_distances* distances, float fill,
+                        const tt_emb_pairs* in, const tt_emb_pairs* out, void* hip_stream) {
+  if (!good_matrix(table, int64_t(1) << 31) || !good_distances(distances) || std::isnan(fill) || !good_pairs(out) ||
+      out->heads != table->cols)
+    return TT_EMB_EINVAL;
+  if (in != nullptr && (!good_pairs(in) || in->batch != out->batch || in->heads != out->heads ||
+                        in->queries != out->queries || in->keys != out->keys))
+    return TT_EMB_EINVAL;
+  if (no_pairs(*out)) return TT_EMB_OK;
+  launch_bias(*table, *distances, fill, in, *out, (hipStream_t)hip_stream);
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? TT_EMB_OK : hip_fail(e);
+}
+
+static size_t sums_bytes(const tt_emb_pairs& g, int span, bool offsets) {
+  const SumPlan p = sum_plan(g, span, offsets);
+  return ((size_t)(p.parts * p.width) * sizeof(float) + 255) & ~(size_t)255;
+}
+
+int tt_emb_bias_workspace_bytes(const tt_emb_pairs* grad, int32_t span, size_t* bytes) {
+  if (bytes == nullptr || !good_sizes(grad) || span < 0 || span > 1 << 20) return TT_EMB_EINVAL;
+  *bytes = std::max(sums_bytes(*grad, span, false), sums_bytes(*grad, span, true));
+  return TT_EMB_OK;
+}
+
+int tt_emb_bias_backward(const tt_emb_pairs* grad, const tt_emb_distances* distances, const tt_emb_matrix* dtable, int add,
+                         void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (!good_pairs(grad) || !good_distances(distances) || !good_matrix(dtable, int64_t(1) << 31) ||
+      grad->heads != dtable->cols)
+    return TT_EMB_EINVAL;
+  const size_t needed = sums_bytes(*grad, distances->span, distances->offsets != nullptr);
+  if (needed > 0) {
+    const int rc = check_workspace(workspace, workspace_bytes, needed);
+    if (rc != TT_EMB_OK) return rc;
+  }
+  if (dtable->rows == 0) return TT_EMB_OK;
+  launch_bias_sums(*grad, *distances, *dtable, add != 0, (float*)workspace, (hipStream_t)hip_stream);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? TT_EMB_OK : hip_fail(e);
 }

@@ -10,45 +10,6 @@ namespace ttemb {
 constexpr int kDenseThreads = 256;
 constexpr int kRowsAhead = 2;  // rows of a lookup that a thread has under way
 
-// Values that a thread takes at once: 16 bytes of the type that is read.  VEC = 1: rows shorter than that.
-// Rows start wherever their strides put them, so these vectors are aligned like single values.
-template <class T, int VEC>
-struct Piece {
-  typedef T V __attribute__((ext_vector_type(VEC), aligned(sizeof(T))));
-};
-template <class T>
-struct Piece<T, 1> {
-  typedef T V;
-};
-
-template <int VEC, class T>
-__device__ __forceinline__ void values_of(const typename Piece<T, VEC>::V& v, float (&x)[VEC]) {
-  if constexpr (VEC == 1) {
-    x[0] = (float)v;
-  } else {
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) x[i] = (float)v[i];
-  }
-}
-
-template <int VEC, class T>
-__device__ __forceinline__ void load_piece(const T* p, float (&x)[VEC]) {
-  values_of<VEC, T>(*(const typename Piece<T, VEC>::V*)p, x);
-}
-
-template <int VEC, class T, bool PAST = false>
-__device__ __forceinline__ void store_piece(T* p, const float (&x)[VEC]) {
-  typename Piece<T, VEC>::V v;
-  if constexpr (VEC == 1) {
-    v = (T)x[0];
-  } else {
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) v[i] = (T)x[i];
-  }
-  if constexpr (PAST) __builtin_nontemporal_store(v, (typename Piece<T, VEC>::V*)p);
-  else *(typename Piece<T, VEC>::V*)p = v;
-}
-
 // How a block's threads are dealt: 2^lanes of them side by side along a row, blockIdx.y over what is left of it.
 struct Lanes {
   int lanes;   // log2
@@ -492,15 +453,6 @@ __global__ __launch_bounds__(kFewThreads) void k_dense_few(TableSource src, int 
 
 // ---------------------------------------------------------------------------------------------
 // host-side launchers
-
-template <class F>
-static void with_type(int type, F&& f) {
-  switch (type) {
-    case TT_EMB_BF16: f(__bf16{}); break;
-    case TT_EMB_FP16: f(_Float16{}); break;
-    default: f(float{}); break;
-  }
-}
 
 // f gets the number of values of a piece: 16 bytes of a type, or one where the rows are shorter
 template <class T, class F>

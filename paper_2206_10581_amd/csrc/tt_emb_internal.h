@@ -533,4 +533,82 @@ __device__ __forceinline__ f4 quad_turned(f4 v, int lane) {
   return upper ? f4{c, d, v.z, v.w} : f4{v.x, v.y, c, d};
 }
 
+// Values that a thread takes at once: 16 bytes of the type that is read.  VEC = 1: rows shorter than that.
+// Rows start wherever their strides put them, so these vectors are aligned like single values.
+template <class T, int VEC>
+struct Piece {
+  typedef T V __attribute__((ext_vector_type(VEC), aligned(sizeof(T))));
+};
+template <class T>
+struct Piece<T, 1> {
+  typedef T V;
+};
+
+template <int VEC, class T>
+__device__ __forceinline__ void values_of(const typename Piece<T, VEC>::V& v, float (&x)[VEC]) {
+  if constexpr (VEC == 1) {
+    x[0] = (float)v;
+  } else {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) x[i] = (float)v[i];
+  }
+}
+
+template <int VEC, class T>
+__device__ __forceinline__ void load_piece(const T* p, float (&x)[VEC]) {
+  values_of<VEC, T>(*(const typename Piece<T, VEC>::V*)p, x);
+}
+
+template <int VEC, class T, bool PAST = false>
+__device__ __forceinline__ void store_piece(T* p, const float (&x)[VEC]) {
+  typename Piece<T, VEC>::V v;
+  if constexpr (VEC == 1) {
+    v = (T)x[0];
+  } else {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) v[i] = (T)x[i];
+  }
+  if constexpr (PAST) __builtin_nontemporal_store(v, (typename Piece<T, VEC>::V*)p);
+  else *(typename Piece<T, VEC>::V*)p = v;
+}
+
+// Rows of logits (tt_emb_tokens.hip), c = scale / log 2; what is written for them; and sums and lists of the parts of a
+// few rows, in the workspace: at most kTokenParts in all, kWave a row.
+struct TokenRows {
+  const void* logits;
+  int64_t ld, rows;
+  int cols;
+  const int64_t* tokens;  // null: all rows count
+  float scale, c;
+};
+struct TokenOut {
+  float *logprob, *entropy, *state;
+  int64_t* top_ids;  // null: no list, and top = 0
+  float* top_logprob;
+  int top;
+};
+struct TokenParts {
+  f4* sums;
+  unsigned long long* lists;
+};
+constexpr int kTokenParts = 512;
+
+// Partial sums of a position bias's gradient (tt_emb_bias.hip): a part is a block's sums over the diagonals of `rows` rows
+// of one head and `group` sequences; a head has groups * chunks of them.
+struct SumPlan {
+  int64_t parts, width;  // all parts, values of each
+  int group, groups, rows, chunks;
+};
+constexpr int kSumParts = 2048;  // about as many at most
+
+inline int type_size(int type) { return type == TT_EMB_FP32 ? 4 : 2; }
+
+// Types of matrices by number: f(T{}) for the type that `type` names.
+template <class F>
+inline void with_type(int type, F&& f) {
+  if (type == TT_EMB_BF16) f(__bf16{});
+  else if (type == TT_EMB_FP16) f(_Float16{});
+  else f(float{});
+}
+
 }  // namespace ttemb
