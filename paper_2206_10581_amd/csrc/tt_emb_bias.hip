@@ -29,22 +29,22 @@ __device__ __forceinline__ float any_value(const tt_emb_matrix& m, int64_t at) {
 
 // ---- bias of tiles
 
-constexpr int kBiasThreads = 256, kBiasCols = 1024, kBiasRows = 64;
-constexpr int kBiasLine = kBiasCols + kBiasRows + 8;  // diagonals of a tile, and some more
+constexpr int kBiasThreads = 256, kBiasAhead = 4;  // rows of a tile that a thread has under way
 struct BiasTiles {
-  int rows, cols;  // of a tile; rows + cols below kBiasLine - 7
+  int rows, cols;  // of a tile
   int down, across;
   int64_t count;
   int lanes;       // log2 of the threads side by side
+  int line;        // places of a line: rows + cols and some more, a multiple of 4
 };
 
-// A block takes a tile of one head.  Its diagonals' values come first, four copies of the line, each a place further, so
-// that any row finds its values in 16-byte words of one of them.
+// A block takes a tile of one head.  Its diagonals' values come first, four copies of the line, each a place further, so that
+// any row finds its values in 16-byte words of one of them; a tile beyond the span has one value.
 template <class TI, class TO, bool ADD>
 __global__ __launch_bounds__(kBiasThreads) void k_bias_tiles(tt_emb_matrix table, tt_emb_distances dist, float fill,
                                                              tt_emb_pairs in, tt_emb_pairs out, BiasTiles tl) {
-  __shared__ __attribute__((aligned(16))) float line[4][kBiasLine];
-  constexpr int P = 16 / (ADD && sizeof(TI) > sizeof(TO) ? sizeof(TI) : sizeof(TO));
+  extern __shared__ __attribute__((aligned(16))) float lines[];
+  constexpr int P = 16 / (ADD && sizeof(TI) > sizeof(TO) ? sizeof(TI) : sizeof(TO)), R = kBiasAhead;
   const int side = threadIdx.x & ((1 << tl.lanes) - 1), up = threadIdx.x >> tl.lanes, step = kBiasThreads >> tl.lanes;
   for (int64_t tile = blockIdx.x; tile < tl.count; tile += gridDim.x) {
     const int64_t plane = tile / ((int64_t)tl.down * tl.across);
@@ -53,43 +53,67 @@ __global__ __launch_bounds__(kBiasThreads) void k_bias_tiles(tt_emb_matrix table
     const int i0 = (int)(place / tl.across) * tl.rows, j0 = (int)(place % tl.across) * tl.cols;
     const int rows = (int)min((int64_t)tl.rows, out.queries - i0), cols = (int)min((int64_t)tl.cols, out.keys - j0);
     const int64_t first = offset_of(dist, b) + j0 - i0 - (rows - 1);  // distance of the first diagonal
-    for (int x = threadIdx.x; x < rows + cols - 1; x += kBiasThreads) {
-      const int u = dist.bucket_of[cut(first + x, dist.span) + dist.span];
-      const float v = (uint32_t)u < (uint32_t)table.rows ? any_value(table, u * table.ld + h) : fill;
+    auto value = [&](int64_t distance) {
+      const int u = dist.bucket_of[cut(distance, dist.span) + dist.span];
+      return (uint32_t)u < (uint32_t)table.rows ? any_value(table, u * table.ld + h) : fill;
+    };
+    const bool one = first >= dist.span || first + rows + cols - 2 <= -dist.span;
+    float all = 0.f;
+    if (one) {
+      all = value(first);
+    } else {
+      for (int x = threadIdx.x; x < rows + cols - 1; x += kBiasThreads) {
+        const float v = value(first + x);
 #pragma unroll
-      for (int s = 0; s < 4; ++s)
-        if (x >= s) line[s][x - s] = v;
+        for (int s = 0; s < 4; ++s)
+          if (x >= s) lines[s * tl.line + x - s] = v;
+      }
+      __syncthreads();
     }
-    __syncthreads();
     const TI* from = (const TI*)in.data + (ADD ? b * in.batch_ld + h * in.head_ld + i0 * in.query_ld + j0 : 0);
     TO* to = (TO*)out.data + b * out.batch_ld + h * out.head_ld + i0 * out.query_ld + j0;
-    for (int r = up; r < rows; r += step)
+    for (int r0 = up; r0 < rows; r0 += step * R)
       for (int c = side * P; c < cols; c += P << tl.lanes) {
-        const int a = c - r + rows - 1, s = a & 3;
-        float v[P];
-        if (c + P <= cols) {
+        if (c + P > cols) {  // cut off
+          for (int r = r0; r < rows && r < r0 + step * R; r += step)
+            for (int i = c; i < cols; ++i) {
+              float y = one ? all : lines[i - r + rows - 1];
+              if constexpr (ADD) y = isinf(y) ? y : (float)from[r * in.query_ld + i] + y;
+              to[r * out.query_ld + i] = (TO)y;
+            }
+          continue;
+        }
+        typename Piece<TI, P>::V v[R];
+        if constexpr (ADD) {
 #pragma unroll
-          for (int i = 0; i < P; i += 4) {
-            const f4 w = *(const f4*)&line[s][a - s + i];
+          for (int k = 0; k < R; ++k)
+            v[k] = *(const typename Piece<TI, P>::V*)(from + min(r0 + k * step, rows - 1) * in.query_ld + c);
+        }
 #pragma unroll
-            for (int k = 0; k < 4; ++k) v[i + k] = w[k];
+        for (int k = 0; k < R; ++k) {
+          const int r = r0 + k * step;
+          if (r >= rows) continue;
+          float y[P];
+          if (one) {
+#pragma unroll
+            for (int i = 0; i < P; ++i) y[i] = all;
+          } else {
+            const int a = c - r + rows - 1, s = a & 3;
+#pragma unroll
+            for (int i = 0; i < P; i += 4) {
+              const f4 w = *(const f4*)&lines[s * tl.line + a - s + i];
+#pragma unroll
+              for (int n = 0; n < 4; ++n) y[i + n] = w[n];
+            }
           }
           if constexpr (ADD) {
-            float x[P];
-            load_piece<P, TI>(from + r * in.query_ld + c, x);
 #pragma unroll
-            for (int i = 0; i < P; ++i) v[i] = isinf(v[i]) ? v[i] : x[i] + v[i];
+            for (int i = 0; i < P; ++i) y[i] = isinf(y[i]) ? y[i] : (float)v[k][i] + y[i];
           }
-          store_piece<P, TO, true>(to + r * out.query_ld + c, v);
-        } else {
-          for (int i = 0; c + i < cols; ++i) {
-            float y = line[0][a + i];
-            if constexpr (ADD) y = isinf(y) ? y : (float)from[r * in.query_ld + c + i] + y;
-            to[r * out.query_ld + c + i] = (TO)y;
-          }
+          store_piece<P, TO, ADD>(to + r * out.query_ld + c, y);
         }
       }
-    __syncthreads();
+    if (!one) __syncthreads();
   }
 }
 
@@ -113,15 +137,27 @@ __device__ __forceinline__ float wave_sum(float v) {
   return v;
 }
 
+// Where a gradient's memory starts and ends: pieces may reach over a row's ends, but not over these.
+template <class T>
+struct Extent {
+  const T *low, *high;
+  __device__ __forceinline__ explicit Extent(const tt_emb_pairs& g) : low((const T*)g.data) {
+    high = low + (g.batch - 1) * g.batch_ld + (g.heads - 1) * g.head_ld + (g.queries - 1) * g.query_ld + g.keys;
+  }
+};
+
 // A block sums the diagonals of some rows of one head and of p.group sequences, a lane B of them at a time: its accumulators
 // stay, the row's place moves by a value from one row to the next.  All before the first and behind the last
-// diagonal are summed apart, row by row.  Fp32 sums of at most a few hundred values.
+// diagonal are summed apart, row by row.
 template <class T, int B>
 __global__ __launch_bounds__(kSumThreads) void k_bias_sums(tt_emb_pairs g, tt_emb_distances dist, int buckets, SumPlan p,
                                                            float* __restrict__ parts) {
+  typedef typename Piece<T, 16 / sizeof(T)>::V VF;
+  typedef typename Piece<T, B>::V VB;
   constexpr int P = 16 / sizeof(T), R = kSumAhead;
   __shared__ float sums[kSumWaves][kWave * B];
-  const int lane = threadIdx.x % kWave, w = threadIdx.x / kWave;
+  const int lane = threadIdx.x % kWave, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+  const Extent<T> all(g);
   for (int64_t part = blockIdx.x; part < p.parts; part += gridDim.x) {
     const int64_t plane = part / p.chunks;
     const int chunk = (int)(part - plane * p.chunks);
@@ -136,43 +172,52 @@ __global__ __launch_bounds__(kSumThreads) void k_bias_sums(tt_emb_pairs g, tt_em
     };
     const bool low = wanted(d.first), high = wanted(d.last);
     float before = 0.f, behind = 0.f;
+    // columns [0, i + until) of row i are before, [i + since, keys) behind
+    const int until = d.first + 1, since = max(d.last, d.first + 1);
     for (int b = b0; b < b1; ++b) {
       const T* rows = (const T*)g.data + b * g.batch_ld + h * g.head_ld;
       for (int i = i0 + w * R; i < i1; i += kSumWaves * R) {
-        // columns [0, until) of a row are before, [since, keys) behind
-        int until[R], since[R];
+        const int n = min(R, i1 - i), most = low ? i + n - 1 + until : 0, least = high ? i + since : keys;
+        for (int c0 = 0; c0 < keys; c0 += kWave * P) {
+          if (c0 >= most && c0 + kWave * P <= least) continue;  // nothing of the group is wanted in any row
+          const int c = c0 + lane * P;
+          const T* at = rows + i * g.query_ld + c;
+          if (n == R && c0 + kWave * P <= keys && (c0 + kWave * P <= (low ? i + until : 0) || c0 >= (high ? i + R - 1 + since : keys))) {
+            VF v[R];
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-          const bool there = i + r < i1;
-          until[r] = there && low ? min(max(i + r + d.first + 1, 0), keys) : 0;
-          since[r] = there && high ? min(max(i + r + max(d.last, d.first + 1), 0), keys) : keys;
-        }
-        for (int c = lane * P; c < keys; c += kWave * P) {
-          typename Piece<T, P>::V v[R];
-          const bool whole = c + P <= keys;
+            for (int r = 0; r < R; ++r) v[r] = *(const VF*)(at + r * g.query_ld);
+            float s[R];
 #pragma unroll
-          for (int r = 0; r < R; ++r)
-            if (whole && (c < until[r] || c + P > since[r]))
-              v[r] = *(const typename Piece<T, P>::V*)(rows + (i + r) * g.query_ld + c);
+            for (int r = 0; r < R; ++r) {
+              s[r] = (float)v[r][0];
+#pragma unroll
+              for (int k = 1; k < P; ++k) s[r] += (float)v[r][k];
+            }
+            float sum = s[0];
+#pragma unroll
+            for (int r = 1; r < R; ++r) sum += s[r];
+            if (c0 < most) before += sum;
+            else behind += sum;
+            continue;
+          }
+          VF v[R];
+          bool whole[R];
 #pragma unroll
           for (int r = 0; r < R; ++r) {
-            if (!(c < until[r] || c + P > since[r])) continue;
-            float a = 0.f, z = 0.f;
-            if (whole) {
+            whole[r] = r < n && c < keys && at + r * g.query_ld + P <= all.high;
+            if (whole[r]) v[r] = *(const VF*)(at + r * g.query_ld);
+          }
 #pragma unroll
-              for (int k = 0; k < P; ++k) {
-                a += c + k < until[r] ? (float)v[r][k] : 0.f;
-                z += c + k >= since[r] ? (float)v[r][k] : 0.f;
-              }
-            } else {
-              for (int k = 0; c + k < keys; ++k) {
-                const float x = (float)rows[(i + r) * g.query_ld + c + k];
-                a += c + k < until[r] ? x : 0.f;
-                z += c + k >= since[r] ? x : 0.f;
-              }
+          for (int r = 0; r < R; ++r) {
+            if (r >= n || c >= keys) continue;
+            const int u = low ? i + r + until : 0, s = high ? i + r + since : keys;
+#pragma unroll
+            for (int k = 0; k < P; ++k) {
+              if (c + k >= keys || (c + k >= u && c + k < s)) continue;
+              const float x = whole[r] ? (float)v[r][k] : (float)at[r * g.query_ld + k];
+              before += c + k < u ? x : 0.f;
+              behind += c + k < u ? 0.f : x;
             }
-            before += a;
-            behind += z;
           }
         }
       }
@@ -198,32 +243,43 @@ __global__ __launch_bounds__(kSumThreads) void k_bias_sums(tt_emb_pairs g, tt_em
       }
     }
     __syncthreads();
-    for (int x0 = d.first + 1; x0 < d.last; x0 += kWave * B) {
-      const int x = x0 + lane * B;  // this lane's first diagonal
+    // what lies between, as far as these rows reach
+    const int end = min(d.last, keys - i0);
+    for (int x0 = max(d.first + 1, 1 - i1); x0 < end; x0 += kWave * B) {
+      const int x = x0 + lane * B;  // this lane's first diagonal; what it sums beyond the end is left
       float acc[B] = {};
       for (int b = b0; b < b1; ++b) {
         const T* rows = (const T*)g.data + b * g.batch_ld + h * g.head_ld;
         // rows that meet the band at all
         const int from = max(i0, -(x0 + kWave * B - 1)), to = (int)min((int64_t)i1, (int64_t)keys - x0);
         for (int i = from + w * R; i < to; i += kSumWaves * R) {
-          typename Piece<T, B>::V v[R];
+          const T* at = rows + i * g.query_ld + (i + x);  // a row on is a column on
+          VB v[R];
+          bool some[R], whole[R], inside = true;
 #pragma unroll
           for (int r = 0; r < R; ++r) {
             const int j = i + r + x;
-            if (i + r < to && j >= 0 && j + B <= keys && x + B <= d.last)
-              v[r] = *(const typename Piece<T, B>::V*)(rows + (i + r) * g.query_ld + j);
+            const T* q = at + r * (g.query_ld + 1);
+            some[r] = i + r < to && j + B > 0 && j < keys;
+            whole[r] = some[r] && q >= all.low && q + B <= all.high;
+            inside = inside && whole[r] && j >= 0 && j + B <= keys;
+            if (whole[r]) v[r] = *(const VB*)q;
+          }
+          if (__all(inside)) {
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+              for (int k = 0; k < B; ++k) acc[k] += (float)v[r][k];
+            continue;
           }
 #pragma unroll
           for (int r = 0; r < R; ++r) {
+            if (!some[r]) continue;
             const int j = i + r + x;
-            if (i + r >= to) continue;
-            if (j >= 0 && j + B <= keys && x + B <= d.last) {
 #pragma unroll
-              for (int k = 0; k < B; ++k) acc[k] += (float)v[r][k];
-            } else {
-#pragma unroll
-              for (int k = 0; k < B; ++k)
-                if (j + k >= 0 && j + k < keys && x + k < d.last) acc[k] += (float)rows[(i + r) * g.query_ld + j + k];
+            for (int k = 0; k < B; ++k) {
+              if (j + k < 0 || j + k >= keys) continue;
+              acc[k] += whole[r] ? (float)v[r][k] : (float)at[r * (g.query_ld + 1) + k];
             }
           }
         }
@@ -231,8 +287,9 @@ __global__ __launch_bounds__(kSumThreads) void k_bias_sums(tt_emb_pairs g, tt_em
 #pragma unroll
       for (int k = 0; k < B; ++k) sums[w][lane * B + k] = acc[k];
       __syncthreads();
-      for (int k = threadIdx.x; k < kWave * B && x0 + k < d.last; k += kSumThreads) {
+      for (int k = threadIdx.x; k < kWave * B && x0 + k < end; k += kSumThreads) {
         float s = 0.f;
+#pragma unroll
         for (int n = 0; n < kSumWaves; ++n) s += sums[n][k];
         out[x0 + k - d.first] = s;
       }
@@ -241,60 +298,90 @@ __global__ __launch_bounds__(kSumThreads) void k_bias_sums(tt_emb_pairs g, tt_em
   }
 }
 
-// A block adds up all parts of one bucket and head.
-template <class TO>
-__global__ __launch_bounds__(kSumThreads) void k_bias_buckets(tt_emb_pairs g, tt_emb_distances dist, SumPlan p,
-                                                              const float* __restrict__ parts, TO* __restrict__ out,
-                                                              int64_t ld, int buckets, bool add) {
-  __shared__ int found[kSumThreads], counts[kSumWaves];
-  __shared__ double sums[kSumWaves];
-  const int lane = threadIdx.x % kWave, w = threadIdx.x / kWave, distances = 2 * dist.span + 1;
-  const int per_head = p.groups * p.chunks;
-  for (int64_t place = blockIdx.x; place < (int64_t)buckets * g.heads; place += gridDim.x) {
-    const int u = (int)(place / g.heads), h = (int)(place - (int64_t)u * g.heads);
+// total[distance][head]: all parts of a head and distance, in fp64.  A block has 64 distances, a wavefront every 16th part.
+constexpr int kJoinThreads = 1024, kJoinWaves = kJoinThreads / kWave, kJoinAhead = 4;
+__global__ __launch_bounds__(kJoinThreads) void k_bias_join(tt_emb_pairs g, tt_emb_distances dist, SumPlan p,
+                                                            const float* __restrict__ parts, double* __restrict__ total) {
+  __shared__ double sums[kJoinWaves][kWave];
+  const int lane = threadIdx.x % kWave, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+  const int per_head = p.groups * p.chunks, distances = 2 * dist.span + 1;
+  const int64_t tiles = (distances + kWave - 1) / kWave;
+  for (int64_t tile = blockIdx.x; tile < tiles * g.heads; tile += gridDim.x) {
+    const int h = (int)(tile / tiles), r = (int)(tile - h * tiles) * kWave + lane, distance = r - dist.span;
     double sum = 0.0;
-    for (int r0 = 0; r0 < distances && per_head > 0; r0 += kSumThreads) {
-      const int r = r0 + (int)threadIdx.x;
-      const uint64_t mask = __ballot(r < distances && dist.bucket_of[min(r, distances - 1)] == u);
-      if (lane == 0) counts[w] = __popcll(mask);
-      __syncthreads();
-      int before = 0, n = 0;
-      for (int k = 0; k < kSumWaves; ++k) {
-        before += k < w ? counts[k] : 0;
-        n += counts[k];
-      }
-      if (mask >> lane & 1) found[before + __popcll(mask & ((uint64_t(1) << lane) - 1))] = r - dist.span;
-      __syncthreads();
-      if (n > 0) {
-        int lanes = 0;
-        while ((1 << lanes) < n) ++lanes;
-        const int m = threadIdx.x & ((1 << lanes) - 1);
-        if (m < n)
-          for (int k = threadIdx.x >> lanes; k < per_head; k += kSumThreads >> lanes) {
-            const int64_t offset = offset_of(dist, k / p.chunks * p.group);
-            const Span d = span_of(g, offset, dist.span);
-            // the diagonal of this distance, if it is told apart or is an end
-            int64_t diagonal = found[m] - offset;
-            if (found[m] == -dist.span && d.first + offset <= -dist.span) diagonal = d.first;
-            else if (found[m] == dist.span && d.last + offset >= dist.span) diagonal = d.last;
-            if (diagonal >= d.first && diagonal <= d.last)
-              sum += (double)parts[((int64_t)h * per_head + k) * p.width + (diagonal - d.first)];
-          }
-      }
-      __syncthreads();
-    }
+    for (int k0 = w; k0 < per_head; k0 += kJoinWaves * kJoinAhead) {
+      float v[kJoinAhead];
+      bool is[kJoinAhead];
 #pragma unroll
-    for (int k = kWave / 2; k > 0; k /= 2) sum += __shfl_xor(sum, k);
-    if (lane == 0) sums[w] = sum;
+      for (int n = 0; n < kJoinAhead; ++n) {
+        const int k = min(k0 + n * kJoinWaves, per_head - 1), group = k / p.chunks, chunk = k - group * p.chunks;
+        const int64_t offset = offset_of(dist, group * p.group);
+        const Span d = span_of(g, offset, dist.span);
+        // the diagonal of this distance; the ends stand for more than their own
+        int64_t diagonal = distance - offset;
+        const bool end = (distance == -dist.span && d.first + offset <= distance) ||
+                         (distance == dist.span && d.last + offset >= distance);
+        if (end) diagonal = distance == -dist.span && d.first + offset <= distance ? d.first : d.last;
+        // what the part's rows do not reach is not written
+        const int64_t i0 = (int64_t)chunk * p.rows, i1 = min(i0 + p.rows, g.queries);
+        is[n] = k0 + n * kJoinWaves < per_head && r < distances && diagonal >= d.first && diagonal <= d.last &&
+                (diagonal == d.first || diagonal == d.last || (diagonal > -i1 && diagonal < g.keys - i0));
+        v[n] = is[n] ? parts[((int64_t)h * per_head + k) * p.width + (diagonal - d.first)] : 0.f;
+      }
+#pragma unroll
+      for (int n = 0; n < kJoinAhead; ++n) sum += is[n] ? (double)v[n] : 0.0;
+    }
+    sums[w][lane] = sum;
     __syncthreads();
-    if (threadIdx.x == 0) {
+    if (w == 0 && r < distances) {
       sum = 0.0;
-      for (int k = 0; k < kSumWaves; ++k) sum += sums[k];
-      TO* to = out + u * ld + h;
-      *to = (TO)(float)(add ? (double)(float)*to + sum : sum);
+#pragma unroll
+      for (int k = 0; k < kJoinWaves; ++k) sum += sums[k][lane];
+      total[(int64_t)r * g.heads + h] = sum;
     }
     __syncthreads();
   }
+}
+
+// A block adds up the distances of one bucket, threads side by side over the heads.
+template <class TO>
+__global__ __launch_bounds__(kSumThreads) void k_bias_buckets(int heads, tt_emb_distances dist, const double* __restrict__ total,
+                                                              TO* __restrict__ out, int64_t ld, int buckets, bool add,
+                                                              int lanes) {
+  __shared__ int found[kSumThreads], counts[kSumWaves];
+  __shared__ double sums[kSumThreads];
+  const int lane = threadIdx.x % kWave, w = threadIdx.x / kWave, distances = total ? 2 * dist.span + 1 : 0;
+  const int side = threadIdx.x & ((1 << lanes) - 1), up = threadIdx.x >> lanes, step = kSumThreads >> lanes;
+  for (int u = blockIdx.x; u < buckets; u += gridDim.x)
+    for (int h0 = 0; h0 < heads; h0 += 1 << lanes) {
+      const int h = h0 + side;
+      double sum = 0.0;
+      for (int r0 = 0; r0 < distances; r0 += kSumThreads) {
+        const int r = r0 + (int)threadIdx.x;
+        const uint64_t mask = __ballot(dist.bucket_of[min(r, distances - 1)] == u && r < distances);
+        if (lane == 0) counts[w] = __popcll(mask);
+        __syncthreads();
+        int before = 0, n = 0;
+#pragma unroll
+        for (int k = 0; k < kSumWaves; ++k) {
+          before += k < w ? counts[k] : 0;
+          n += counts[k];
+        }
+        if (mask >> lane & 1) found[before + __popcll(mask & ((uint64_t(1) << lane) - 1))] = r;
+        __syncthreads();
+        if (h < heads)
+          for (int m = up; m < n; m += step) sum += total[(int64_t)found[m] * heads + h];
+        __syncthreads();
+      }
+      sums[threadIdx.x] = sum;
+      __syncthreads();
+      if (up == 0 && h < heads) {
+        for (int k = 1; k < step; ++k) sum += sums[(k << lanes) + side];
+        TO* to = out + u * ld + h;
+        *to = (TO)(float)(add ? (double)(float)*to + sum : sum);
+      }
+      __syncthreads();
+    }
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -305,26 +392,27 @@ constexpr int64_t kMostBlocks = 1 << 20;
 void launch_bias(const tt_emb_matrix& table, const tt_emb_distances& dist, float fill, const tt_emb_pairs* in,
                  const tt_emb_pairs& out, hipStream_t st) {
   BiasTiles tl;
-  const int size = type_size(std::min(out.type, in ? in->type : out.type)), P = 16 / size;
-  tl.cols = (int)std::min<int64_t>((out.keys + P - 1) / P * P, kBiasCols);
-  tl.across = (int)((out.keys + tl.cols - 1) / tl.cols);
+  const int size = std::max(type_size(out.type), in ? type_size(in->type) : 0), P = 16 / size;
   const int64_t planes = (int64_t)out.batch * out.heads;
-  tl.rows = (int)std::min<int64_t>(std::min<int64_t>(out.queries, kBiasLine - 8 - tl.cols), 65536 / tl.cols);
+  tl.cols = (int)std::min<int64_t>((out.keys + P - 1) / P * P, out.queries <= 8 ? 2048 : 1024);
+  tl.across = (int)((out.keys + tl.cols - 1) / tl.cols);
+  tl.rows = (int)std::min<int64_t>(std::min<int64_t>(out.queries, 1088 - std::min(tl.cols, 1024)), 65536 / tl.cols);
   // enough tiles for all compute units
   while (tl.rows > 8 && planes * tl.across * ((out.queries + tl.rows - 1) / tl.rows) < 2048) tl.rows /= 2;
   tl.down = (int)((out.queries + tl.rows - 1) / tl.rows);
   tl.count = planes * tl.down * tl.across;
   tl.lanes = 0;
   while ((1 << tl.lanes) < kBiasThreads && (P << tl.lanes) < tl.cols) ++tl.lanes;
-  const int blocks = (int)std::min(tl.count, kMostBlocks);
+  tl.line = (tl.rows + tl.cols + 11) / 4 * 4;
+  const int blocks = (int)std::min(tl.count, kMostBlocks), lds = 4 * tl.line * (int)sizeof(float);
   with_type(out.type, [&](auto to) {
     typedef decltype(to) TO;
     if (in == nullptr) {
-      k_bias_tiles<TO, TO, false><<<blocks, kBiasThreads, 0, st>>>(table, dist, fill, out, out, tl);
+      k_bias_tiles<TO, TO, false><<<blocks, kBiasThreads, lds, st>>>(table, dist, fill, out, out, tl);
       return;
     }
     with_type(in->type, [&](auto ti) {
-      k_bias_tiles<decltype(ti), TO, true><<<blocks, kBiasThreads, 0, st>>>(table, dist, fill, *in, out, tl);
+      k_bias_tiles<decltype(ti), TO, true><<<blocks, kBiasThreads, lds, st>>>(table, dist, fill, *in, out, tl);
     });
   });
 }
@@ -334,9 +422,9 @@ SumPlan sum_plan(const tt_emb_pairs& g, int span, bool offsets) {
   const int64_t batch = g.batch, heads = g.heads;
   if (batch == 0 || heads == 0 || g.queries == 0 || g.keys == 0) return p;
   p.width = std::min<int64_t>(g.queries + g.keys - 1, 2 * (int64_t)span + 1);
-  // parts of a head: enough blocks, each with 16 times the values that it leaves
+  // parts of a head: enough blocks, each with eight times the values that it leaves
   const int64_t places = batch * g.queries * g.keys;
-  const int64_t want = std::max<int64_t>(1, std::min<int64_t>(kSumParts / heads, places / (16 * p.width)));
+  const int64_t want = std::max<int64_t>(1, std::min<int64_t>(kSumParts / heads, places / (8 * p.width)));
   p.group = offsets ? 1 : (int)((batch + want - 1) / want);
   p.groups = (int)((batch + p.group - 1) / p.group);
   const int64_t chunks = std::max<int64_t>(1, std::min<int64_t>(want / p.groups, (g.queries + 15) / 16));
@@ -347,9 +435,8 @@ SumPlan sum_plan(const tt_emb_pairs& g, int span, bool offsets) {
 }
 
 void launch_bias_sums(const tt_emb_pairs& g, const tt_emb_distances& dist, const tt_emb_matrix& out, bool add,
-                      float* parts, hipStream_t st) {
-  const SumPlan p = sum_plan(g, dist.span, dist.offsets != nullptr);
-  if (p.parts > 0)
+                      const SumPlan& p, double* total, float* parts, hipStream_t st) {
+  if (p.parts > 0) {
     with_type(g.type, [&](auto t) {
       typedef decltype(t) T;
       const int blocks = (int)std::min(p.parts, kMostBlocks);
@@ -358,11 +445,15 @@ void launch_bias_sums(const tt_emb_pairs& g, const tt_emb_distances& dist, const
       else
         k_bias_sums<T, 8><<<blocks, kSumThreads, 0, st>>>(g, dist, (int)out.rows, p, parts);
     });
-  const int64_t places = out.rows * out.cols;
+    const int64_t tiles = (2 * (int64_t)dist.span + kWave) / kWave * g.heads;
+    k_bias_join<<<(int)std::min(tiles, kMostBlocks), kJoinThreads, 0, st>>>(g, dist, p, parts, total);
+  }
+  int lanes = 0;
+  while ((1 << lanes) < kWave && (1 << lanes) < g.heads) ++lanes;
   with_type(out.type, [&](auto t) {
     typedef decltype(t) TO;
-    k_bias_buckets<TO><<<(int)std::min(places, kMostBlocks), kSumThreads, 0, st>>>(g, dist, p, parts, (TO*)out.data, out.ld,
-                                                                                 (int)out.rows, add);
+    k_bias_buckets<TO><<<(int)std::min(out.rows, kMostBlocks), kSumThreads, 0, st>>>(
+        g.heads, dist, p.parts > 0 ? total : nullptr, (TO*)out.data, out.ld, (int)out.rows, add, lanes);
   });
 }
 

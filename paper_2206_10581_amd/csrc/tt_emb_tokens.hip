@@ -4,6 +4,8 @@
 //   log p = z - log S,   entropy = log S - T / S,   dx = scale (g (1 - p) or -g p  -  h p (log p + entropy)).
 // m, S and T come from one pass: what a thread has summed is rescaled where it meets a larger logit.  z is formed from the difference,
 // so that neither a mask of the type's lowest value nor scale overflows it.  All is bound by the memory.
+#include <limits.h>
+
 #include <algorithm>
 #include <type_traits>
 
@@ -42,18 +44,63 @@ __device__ __forceinline__ void add_values(Sums& s, const float (&x)[N], float m
   }
 }
 
+// Of every 2 D lanes (D = 16 or 32) what the lower and the upper half hold, in both.
+struct Halves {
+  uint32_t lower, upper;
+};
+template <int D>
+__device__ __forceinline__ Halves halves(uint32_t v) {
+  if constexpr (D == 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return {r[0], r[1]};
+  } else {
+    const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return {r[0], r[1]};
+  }
+}
+// What the lane at distance D (a power of two) holds, where groups of D lanes hold the same: f(own, other) in every lane.
+template <int D, class F>
+__device__ __forceinline__ float joined_lanes(float v, F&& f) {
+  const uint32_t b = __builtin_bit_cast(uint32_t, v);
+  if constexpr (D >= 16) {
+    const Halves r = halves<D>(b);
+    return f(__builtin_bit_cast(float, r.lower), __builtin_bit_cast(float, r.upper));
+  } else {  // neighbour, neighbouring pair, mirrored eight, mirrored sixteen
+    constexpr int kMove = D == 1 ? 0xB1 : D == 2 ? 0x4E : D == 4 ? 0x141 : 0x140;
+    return f(v, __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp((int)b, kMove, 0xf, 0xf, true)));
+  }
+}
+template <int L, class F>
+__device__ __forceinline__ float over_lanes(float v, F&& f) {
+  if constexpr (L > 1) v = joined_lanes<1>(v, f);
+  if constexpr (L > 2) v = joined_lanes<2>(v, f);
+  if constexpr (L > 4) v = joined_lanes<4>(v, f);
+  if constexpr (L > 8) v = joined_lanes<8>(v, f);
+  if constexpr (L > 16) v = joined_lanes<16>(v, f);
+  if constexpr (L > 32) v = joined_lanes<32>(v, f);
+  return v;
+}
+template <int L, class F>
+__device__ __forceinline__ uint32_t lanes_of(uint32_t v, F&& f) {
+  return __builtin_bit_cast(uint32_t, over_lanes<L>(__builtin_bit_cast(float, v), [&](float a, float b) {
+                              return __builtin_bit_cast(float, f(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)));
+                            }));
+}
+template <int L>
+__device__ __forceinline__ float lanes_max(float v) {
+  return over_lanes<L>(v, [](float a, float b) { return fmaxf(a, b); });
+}
+template <int L>
+__device__ __forceinline__ float lanes_sum(float v) {
+  return over_lanes<L>(v, [](float a, float b) { return a + b; });
+}
+
 // Over groups of L lanes, the same in every lane of a group.
 template <bool ENT, int L>
 __device__ __forceinline__ void join_lanes(Sums& s, float c) {
-  float most = s.most;
-#pragma unroll
-  for (int d = L / 2; d > 0; d /= 2) most = fmaxf(most, __shfl_xor(most, d));
-  rescale<ENT>(s, most, c);
-#pragma unroll
-  for (int d = L / 2; d > 0; d /= 2) {
-    s.sum += __shfl_xor(s.sum, d);
-    if constexpr (ENT) s.tilt += __shfl_xor(s.tilt, d);
-  }
+  rescale<ENT>(s, lanes_max<L>(s.most), c);
+  s.sum = lanes_sum<L>(s.sum);
+  if constexpr (ENT) s.tilt = lanes_sum<L>(s.tilt);
 }
 
 // Over a block, the same in every thread.  `part`: a place for each wavefront; free again after the caller's next barrier.
@@ -86,92 +133,214 @@ __device__ __forceinline__ Key read_lane(Key k, int lane) {
          (uint32_t)__builtin_amdgcn_readlane((int)k, lane);
 }
 __device__ __forceinline__ Key max_key(Key a, Key b) { return a > b ? a : b; }
-__device__ __forceinline__ Key min_key(Key a, Key b) { return a > b ? b : a; }
 
-// A bitonic sequence of a wavefront's keys into falling order.
-__device__ __forceinline__ Key merged(Key k) {
-  const int lane = threadIdx.x % kWave;
-#pragma unroll
-  for (int d = kWave / 2; d > 0; d /= 2) {
-    const Key o = __shfl_xor(k, d);
-    k = lane & d ? min_key(k, o) : max_key(k, o);
+// What lane ^ D holds.
+template <int D>
+__device__ __forceinline__ uint32_t across(uint32_t v) {
+  if constexpr (D >= 16) {
+    const Halves r = halves<D>(v);
+    return threadIdx.x & D ? r.lower : r.upper;
+  } else if constexpr (D == 4) {  // mirrored eight, then mirrored four
+    const int m = __builtin_amdgcn_mov_dpp((int)v, 0x141, 0xf, 0xf, true);
+    return (uint32_t)__builtin_amdgcn_mov_dpp(m, 0x1B, 0xf, 0xf, true);
+  } else {
+    constexpr int kMove = D == 1 ? 0xB1 : D == 2 ? 0x4E : 0x128;  // the last: eight on, of sixteen
+    return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, kMove, 0xf, 0xf, true);
   }
-  return k;
+}
+template <int D>
+__device__ __forceinline__ Key across(Key k) {
+  return (Key)across<D>((uint32_t)(k >> 32)) << 32 | across<D>((uint32_t)k);
+}
+// One step of a sorting network: pairs at distance D, the larger first in groups of RUN lanes and last in every other.
+template <int D, int RUN>
+__device__ __forceinline__ Key ordered(Key k) {
+  const bool upper = threadIdx.x & D, falling = RUN >= kWave || (threadIdx.x & RUN) == 0;
+  const Key o = across<D>(k);
+  return (k > o) == (upper != falling) ? k : o;
+}
+template <int RUN>
+__device__ __forceinline__ Key merged(Key k) {
+  if constexpr (RUN > 32) k = ordered<32, RUN>(k);
+  if constexpr (RUN > 16) k = ordered<16, RUN>(k);
+  if constexpr (RUN > 8) k = ordered<8, RUN>(k);
+  if constexpr (RUN > 4) k = ordered<4, RUN>(k);
+  if constexpr (RUN > 2) k = ordered<2, RUN>(k);
+  return ordered<1, RUN>(k);
 }
 __device__ __forceinline__ Key sorted(Key k) {
-  const int lane = threadIdx.x % kWave;
-#pragma unroll
-  for (int run = 2; run < kWave; run *= 2)
-#pragma unroll
-    for (int d = run / 2; d > 0; d /= 2) {
-      const Key o = __shfl_xor(k, d);
-      k = ((lane & d) != 0) == ((lane & run) == 0) ? min_key(k, o) : max_key(k, o);
-    }
-  return merged(k);
+  return merged<64>(merged<32>(merged<16>(merged<8>(merged<4>(merged<2>(k))))));
+}
+__device__ __forceinline__ uint32_t mirrored(uint32_t v) {  // lane 63 - l
+  return across<32>(across<16>((uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x140, 0xf, 0xf, true)));
 }
 // The larger half of two falling lists, falling.
 __device__ __forceinline__ Key joined(Key a, Key b) {
-  return merged(max_key(a, __shfl(b, kWave - 1 - (int)(threadIdx.x % kWave))));
+  return merged<64>(max_key(a, (Key)mirrored((uint32_t)(b >> 32)) << 32 | mirrored((uint32_t)b)));
 }
 
-// The largest 64 keys that a wavefront has met, one a lane, falling; what does not exceed the one in lane top - 1 is not
-// put in.
+__device__ __forceinline__ uint32_t lane_place(uint64_t mask) {  // how many lanes of the mask lie below this one
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+}
+
+// x[i] for an i of each lane's own.
+template <int N>
+__device__ __forceinline__ float picked(const float (&x)[N], int i) {
+  if constexpr (N == 1) {
+    return x[0];
+  } else {
+    float half[(N + 1) / 2];
+#pragma unroll
+    for (int k = 0; k < (N + 1) / 2; ++k) {
+      const float even = x[2 * k], odd = x[2 * k + 1 < N ? 2 * k + 1 : 2 * k];
+      half[k] = i & 1 ? odd : even;
+    }
+    return picked<(N + 1) / 2>(half, i >> 1);
+  }
+}
+
+// Keys in LDS, one behind the other, of which a wavefront makes a falling list of 64.
+__device__ __forceinline__ Key listed(const Key* keys, int n) {
+  const int lane = threadIdx.x % kWave;
+  Key list = 0;
+  for (int k = 0; k < n; k += kWave) {
+    const Key next = sorted(k + lane < n ? keys[k + lane] : 0);
+    list = k == 0 ? next : joined(list, next);
+  }
+  return list;
+}
+
+// The largest `top` keys of a row, by the wavefronts of a block.  Each has a list of those that it met, one a lane, falling (what
+// follows the first `top` may be anything smaller); values that may belong to it wait in its share of `room` until there are 64,
+// which are sorted and joined at once.  What is smaller than `least` is not looked at: at least `top` values of the block's first
+// step, or of a step of the wavefront, or of its list are larger.
+constexpr int kWaiting = 2 * kWave;
+template <int NT>
+struct TopRoom {
+  static constexpr int W = NT / kWave;
+  Key waiting[W][kWaiting], together[W * kWaiting], least[W];
+  uint32_t most[NT];
+  int count[W];
+};
+template <int NT>
 struct TopList {
+  static constexpr int W = NT / kWave;
   Key list, least;
   float least_value;
-  int top;
-  __device__ __forceinline__ explicit TopList(int n) : list(0), least(0), least_value(-INFINITY), top(n) {}
-  __device__ __forceinline__ void settle() {
-    least = read_lane(list, top - 1);
-    least_value = least ? key_value(least) : -INFINITY;
+  int top, waiting;
+  bool started;
+  TopRoom<NT>* room;
+  Key* buffer;
+  __device__ __forceinline__ TopList(int n, TopRoom<NT>* r)
+      : list(0), least(0), least_value(-INFINITY), top(n), waiting(0), started(false), room(r),
+        buffer(r->waiting[threadIdx.x / kWave]) {}
+  __device__ __forceinline__ void raise(Key k) {
+    if (k > least) {
+      least = k;
+      least_value = key_value(k);
+    }
   }
-  // One key a lane (0: none).  Few are put in one by one, many sorted and joined.
-  __device__ __forceinline__ void put(Key k) {
-    uint64_t mask = __ballot(k > least);
-    if (__popcll(mask) > 10) {
-      list = joined(list, sorted(k > least ? k : 0));
-      settle();
-      return;
+  // The places of N * 64 values of which at least `top` are not smaller: from the highest bit, as far as bf16 has them.
+  template <int N>
+  __device__ __forceinline__ void raise_to_top_of(const uint32_t (&o)[N]) {
+    uint32_t t = 0;
+#pragma unroll
+    for (int b = 31; b >= 16; --b) {
+      int n = 0;
+#pragma unroll
+      for (int i = 0; i < N; ++i) n += __popcll(__ballot(o[i] >= (t | 1u << b)));
+      if (n >= top) t |= 1u << b;
     }
-    while (mask) {
-      const Key n = read_lane(k, __ffsll((unsigned long long)mask) - 1);
-      Key before = __shfl_up(list, 1);
-      if (threadIdx.x % kWave == 0) before = ~(Key)0;
-      list = list > n ? list : before > n ? n : before;
-      settle();
-      mask &= mask - 1;
-      mask &= __ballot(k > least);
+    raise((Key)t << 32);
+  }
+  __device__ __forceinline__ void join_waiting() {
+    wave_sync();
+    list = joined(list, listed(buffer, waiting));
+    waiting = 0;
+    raise(read_lane(list, top - 1));
+  }
+  __device__ __forceinline__ void wait(Key k, bool in) {
+    const uint64_t mask = __ballot(in);
+    if (in) buffer[waiting + lane_place(mask)] = k;
+    waiting += __popcll(mask);
+  }
+  // N values a lane, their largest, whether there is any and is(i) each, and index(i) of each.  The same steps for all threads
+  // of a block.
+  template <int N, class B, class I>
+  __device__ __forceinline__ void offer(const float (&x)[N], float most, bool nan, bool there, B&& is, I&& index) {
+    if (!started) {
+      room->most[threadIdx.x] = there ? (uint32_t)(key_of(nan ? NAN : most, 0) >> 32) : 0;
+      __syncthreads();
+      uint32_t o[W];
+#pragma unroll
+      for (int w = 0; w < W; ++w) o[w] = room->most[w * kWave + threadIdx.x % kWave];
+      raise_to_top_of(o);
+      started = true;
+    } else {
+      if (!__any(!(most < least_value) || nan)) return;
+      const uint32_t o[1] = {there ? (uint32_t)(key_of(nan ? NAN : most, 0) >> 32) : 0};
+      raise_to_top_of(o);
     }
+    uint32_t may = 0;  // which values may belong to the list
+#pragma unroll
+    for (int i = 0; i < N; ++i) may |= is(i) && !(x[i] < least_value) ? 1u << i : 0;
+    while (__any(may != 0)) {
+      const int i = __ffs(may) - 1;
+      const Key k = may ? key_of(picked<N>(x, i), index(i)) : 0;
+      wait(k, k >= least && k != 0);
+      may &= may - 1;
+      if (waiting >= kWave) join_waiting();
+    }
+  }
+  // The block's list, in its first wavefront.
+  __device__ __forceinline__ Key finish() {
+    const int lane = threadIdx.x % kWave, w = threadIdx.x / kWave;
+    if (lane == 0) room->least[w] = least;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < W; ++k) raise(room->least[k]);
+    wait(list, lane < top && list >= least && list != 0);  // fewer than 64 wait
+    wave_sync();
+    Key keep[kWaiting / kWave];
+    uint64_t mask[kWaiting / kWave];
+    int n = 0;
+#pragma unroll
+    for (int k = 0; k < kWaiting / kWave; ++k) {
+      keep[k] = k * kWave + lane < waiting ? buffer[k * kWave + lane] : 0;
+      mask[k] = __ballot(keep[k] >= least && keep[k] != 0);
+      n += __popcll(mask[k]);
+    }
+    if (lane == 0) room->count[w] = n;
+    __syncthreads();
+    int from = 0, all = 0;
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+      from += k < w ? room->count[k] : 0;
+      all += room->count[k];
+    }
+#pragma unroll
+    for (int k = 0; k < kWaiting / kWave; ++k) {
+      if (mask[k] >> lane & 1) room->together[from + lane_place(mask[k])] = keep[k];
+      from += __popcll(mask[k]);
+    }
+    __syncthreads();
+    return w == 0 ? listed(room->together, all) : 0;
   }
 };
-
-// The lists of W wavefronts joined into the first's.  `lists`: 64 places for each; free again after the next barrier.
-template <int W>
-__device__ __forceinline__ void join_lists(Key& list, Key* lists) {
-  const int lane = threadIdx.x % kWave, w = threadIdx.x / kWave;
-  lists[w * kWave + lane] = list;
-#pragma unroll
-  for (int half = W / 2; half > 0; half /= 2) {
-    __syncthreads();
-    if (w < half) {
-      list = joined(list, lists[(w + half) * kWave + lane]);
-      lists[w * kWave + lane] = list;
-    }
-  }
-}
+struct NoList {};  // in its place where none is wanted
 
 // ---- what is read and written
 
-__device__ __forceinline__ float log_sum(const Sums& s) { return s.sum == 0.f ? -INFINITY : logf(s.sum); }
+// S is 1 at least (the largest logit's own term), or 0: the row is empty.
+__device__ __forceinline__ float log_sum(const Sums& s) { return __builtin_amdgcn_logf(s.sum) * kLn2; }
 
-// One lane of the row's writes the numbers; the first `top` lanes of a wavefront write the list.
-__device__ __forceinline__ void put_numbers(const TokenOut& o, const TokenRows& t, int64_t row, const Sums& s,
-                                            int64_t token, float x) {
+// One lane of the row's writes the numbers, as many lanes as the list is long write that.
+__device__ __forceinline__ void put_numbers(const TokenOut& o, const TokenRows& t, int64_t row, const Sums& s, float x) {
   const float logs = log_sum(s);
   const bool empty = s.sum == 0.f;
   if (o.logprob) o.logprob[row] = empty ? -INFINITY : (x - s.most) * t.scale - logs;
   if (o.entropy) {
-    const float h = logs - s.tilt / s.sum * kLn2;
+    const float h = logs - s.tilt * __builtin_amdgcn_rcpf(s.sum) * kLn2;
     o.entropy[row] = empty || h < 0.f ? 0.f : h;
   }
   if (o.state) {
@@ -199,7 +368,7 @@ struct RowGradient {
   bool zero;      // nothing is read
 };
 __device__ __forceinline__ RowGradient loss_gradient(const TokenRows& t, const Sums& s, float w, int64_t token) {
-  return {s.most, log2f(s.sum), t.scale * w, 0.f, -t.scale * w, token, s.sum == 0.f};
+  return {s.most, __builtin_amdgcn_logf(s.sum), t.scale * w, 0.f, -t.scale * w, token, s.sum == 0.f};
 }
 template <bool ENT>
 __device__ __forceinline__ float gradient_of(const RowGradient& g, float x, int v, float c) {
@@ -240,6 +409,16 @@ struct NarrowRow {
   __device__ __forceinline__ bool mine(int q, int i, int cols) const {
     return first[q] + i >= own[q] && first[q] + i < cols;
   }
+  // The logit of column v, the same in all lanes of the row's.
+  __device__ __forceinline__ float at(int64_t v, int cols) const {
+    float found = -INFINITY;
+#pragma unroll
+    for (int q = 0; q < N; ++q)
+#pragma unroll
+      for (int i = 0; i < P; ++i)
+        if (first[q] + i == v && mine(q, i, cols)) found = x[q * P + i];
+    return lanes_max<L>(found);
+  }
   template <bool ENT>
   __device__ __forceinline__ Sums sums(int cols, float c) const {
     float v[N * P], most = kLowest;
@@ -258,44 +437,72 @@ struct NarrowRow {
 };
 
 constexpr int kNarrowThreads = 256;
+constexpr int kNarrowList = 16;  // most lanes of a row whose list is made here; longer rows are taken by blocks
+template <int N>
+constexpr int kNarrowRows = N > 2 ? 1 : 4 / N;  // that a group of lanes has under way
+
+// Narrow rows with their tokens, all loads before all else: f(row, its token, its logits).
+template <class T, int L, int N, class F>
+__device__ __forceinline__ void narrow_rows(const TokenRows& t, F&& f) {
+  constexpr int R = kNarrowRows<N>, kSide = kNarrowThreads / L;
+  const int lane = threadIdx.x % L;
+  for (int64_t row0 = (int64_t)blockIdx.x * kSide * R + threadIdx.x / L; row0 < t.rows; row0 += (int64_t)gridDim.x * kSide * R) {
+    int64_t token[R];
+    NarrowRow<T, L, N> r[R];
+#pragma unroll
+    for (int j = 0; j < R; ++j) token[j] = t.tokens ? t.tokens[min(row0 + j * kSide, t.rows - 1)] : 0;
+#pragma unroll
+    for (int j = 0; j < R; ++j) r[j].load((const T*)t.logits + min(row0 + j * kSide, t.rows - 1) * t.ld, t.cols, lane);
+#pragma unroll
+    for (int j = 0; j < R; ++j)
+      if (row0 + j * kSide < t.rows) f(row0 + j * kSide, token[j], r[j]);
+  }
+}
+
 template <class T, int L, int N>
 __global__ __launch_bounds__(kNarrowThreads) void k_token_narrow(TokenRows t, TokenOut o) {
   constexpr int P = 16 / sizeof(T);
   const int lane = threadIdx.x % L;
-  const T* x = (const T*)t.logits;
-  for (int64_t row = (int64_t)blockIdx.x * (kNarrowThreads / L) + threadIdx.x / L; row < t.rows;
-       row += (int64_t)gridDim.x * (kNarrowThreads / L)) {
-    const int64_t token = t.tokens ? t.tokens[row] : 0;
+  narrow_rows<T, L, N>(t, [&](int64_t row, int64_t token, const NarrowRow<T, L, N>& r) {
     if ((uint64_t)token >= (uint64_t)t.cols) {
       if (lane == 0) put_none(o, t, row);
       if (o.top_ids)
         for (int k = lane; k < o.top; k += L) put_top(o, t, row, Sums{0.f, 0.f, 0.f}, 0, k);
-      continue;
+      return;
     }
-    NarrowRow<T, L, N> r;
-    r.load(x + row * t.ld, t.cols, lane);
-    const float at = (float)x[row * t.ld + token];
+    const float at = r.at(token, t.cols);
     const Sums s = o.entropy ? r.template sums<true>(t.cols, t.c) : r.template sums<false>(t.cols, t.c);
-    if (lane == 0) put_numbers(o, t, row, s, token, at);
-    if (!o.top_ids) continue;
-    Key last = ~(Key)0;
-    for (int k = 0; k < o.top; ++k) {  // the largest that is smaller than the one before
-      Key best = 0;
-      if (last != 0) {
+    if (lane == 0) put_numbers(o, t, row, s, at);
+    if constexpr (L <= kNarrowList) {
+      if (!o.top_ids) return;
+      // the largest that is left, `top` times: what is taken becomes 0
+      uint32_t left[N * P];
+#pragma unroll
+      for (int q = 0; q < N; ++q)
+#pragma unroll
+        for (int i = 0; i < P; ++i)
+          left[q * P + i] = r.mine(q, i, t.cols) ? (uint32_t)(key_of(r.x[q * P + i], 0) >> 32) : 0;
+      Key mine = 0;  // place k's, in lane k % L
+      for (int k = 0; k < o.top; ++k) {
+        uint32_t best = 0;
+#pragma unroll
+        for (int i = 0; i < N * P; ++i) best = max(best, left[i]);
+        const uint32_t most = lanes_of<L>(best, [](uint32_t a, uint32_t b) { return max(a, b); });
+        uint32_t place = INT_MAX;
+#pragma unroll
+        for (int q = N - 1; q >= 0; --q)
+#pragma unroll
+          for (int i = P - 1; i >= 0; --i) place = left[q * P + i] == most ? (uint32_t)(r.first[q] + i) : place;
+        place = lanes_of<L>(place, [](uint32_t a, uint32_t b) { return min(a, b); });
 #pragma unroll
         for (int q = 0; q < N; ++q)
 #pragma unroll
-          for (int i = 0; i < P; ++i) {
-            const Key n = key_of(r.x[q * P + i], r.first[q] + i);
-            if (r.mine(q, i, t.cols) && n < last) best = max_key(best, n);
-          }
-#pragma unroll
-        for (int d = L / 2; d > 0; d /= 2) best = max_key(best, __shfl_xor(best, d));
+          for (int i = 0; i < P; ++i) left[q * P + i] = r.first[q] + i == (int)place ? 0 : left[q * P + i];
+        if (lane == k % L) mine = most == 0 ? 0 : (Key)most << 32 | ~place;
+        if (k % L == L - 1 || k == o.top - 1) put_top(o, t, row, s, mine, lane <= k % L ? k / L * L + lane : o.top);
       }
-      if (lane == k % L) put_top(o, t, row, s, best, k);
-      last = best;
     }
-  }
+  });
 }
 
 template <class T, class TO, int L, int N>
@@ -304,18 +511,11 @@ __global__ __launch_bounds__(kNarrowThreads) void k_token_loss_narrow(TokenRows 
                                                                       int64_t ld_dx) {
   constexpr int P = 16 / sizeof(T);
   const int lane = threadIdx.x % L;
-  const T* x = (const T*)t.logits;
-  for (int64_t row = (int64_t)blockIdx.x * (kNarrowThreads / L) + threadIdx.x / L; row < t.rows;
-       row += (int64_t)gridDim.x * (kNarrowThreads / L)) {
-    const int64_t token = t.tokens[row];
-    const bool counts = (uint64_t)token < (uint64_t)t.cols;
-    NarrowRow<T, L, N> r;
-    Sums s{0.f, 0.f, 0.f};
+  narrow_rows<T, L, N>(t, [&](int64_t row, int64_t token, const NarrowRow<T, L, N>& r) {
     RowGradient g{};
-    if (counts) {
-      r.load(x + row * t.ld, t.cols, lane);
-      const float at = (float)x[row * t.ld + token];
-      s = r.template sums<false>(t.cols, t.c);
+    if ((uint64_t)token < (uint64_t)t.cols) {
+      const float at = r.at(token, t.cols);
+      const Sums s = r.template sums<false>(t.cols, t.c);
       g = loss_gradient(t, s, weights ? weight * weights[row] : weight, token);
       if (lane == 0) logprob[row] = s.sum == 0.f ? -INFINITY : (at - s.most) * t.scale - log_sum(s);
     } else {
@@ -324,59 +524,70 @@ __global__ __launch_bounds__(kNarrowThreads) void k_token_loss_narrow(TokenRows 
     }
 #pragma unroll
     for (int q = 0; q < N; ++q) {
-      const int own = (q * L + lane) * P, first = t.cols >= P ? min(own, t.cols - P) : 0;
-      if (own >= t.cols) continue;
+      if (r.own[q] >= t.cols) continue;
       float v[P];
 #pragma unroll
-      for (int i = 0; i < P; ++i) v[i] = g.zero ? 0.f : gradient_of<false>(g, r.x[q * P + i], first + i, t.c);
-      TO* to = dx + row * ld_dx + first;
+      for (int i = 0; i < P; ++i) v[i] = g.zero ? 0.f : gradient_of<false>(g, r.x[q * P + i], r.first[q] + i, t.c);
+      TO* to = dx + row * ld_dx + r.first[q];
       if (t.cols >= P) store_piece<P, TO>(to, v);
       else
 #pragma unroll
         for (int i = 0; i < P; ++i)
           if (i < t.cols) to[i] = (TO)v[i];
     }
-  }
+  });
 }
 
 // ---- wide rows: a block has one, or a part of one
 
-// Four pieces of a row at a time by every thread of a block, then what is left of the columns [from, to): f(values,
-// columns of their pieces, how many of them there are a piece).
-template <int NT, class T, class F, class G>
-__device__ __forceinline__ void sweep(const T* __restrict__ row, int from, int to, F&& four, G&& one) {
+// Four pieces of a row at a time by every thread of a block: f(values, first columns of the pieces, how many values of each
+// are not the piece's own, whether there are such).  The last piece of the columns [from, to) starts early where it is cut off;
+// places without a piece hold -infinity.  The row has a piece's width at least.
+template <int U, int NT, class T, class F>
+__device__ __forceinline__ void last_step(const T* __restrict__ row, int from, int to, int k, F&& f) {
+  constexpr int P = 16 / sizeof(T);
+  int first[U], skip[U];
+  typename Piece<T, P>::V v[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int own = from + (k + u * NT) * P;
+    first[u] = min(own, to - P);
+    skip[u] = min(own - first[u], P);
+    v[u] = *(const typename Piece<T, P>::V*)(row + first[u]);
+  }
+  float x[U * P];
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int i = 0; i < P; ++i) x[u * P + i] = i >= skip[u] ? (float)v[u][i] : -INFINITY;
+  f(x, first, skip, std::true_type{});
+}
+template <int NT, class T, class F>
+__device__ __forceinline__ void sweep(const T* __restrict__ row, int from, int to, F&& f) {
   constexpr int P = 16 / sizeof(T), U = 4;
-  const int pieces = (to - from) / P;
-  int k = threadIdx.x;
-  for (; k - (int)threadIdx.x + U * NT <= pieces; k += U * NT) {  // the same for all
+  const int whole = (to - from) / P, pieces = (to - from + P - 1) / P;
+  int k0 = 0;
+  for (; k0 + U * NT <= whole; k0 += U * NT) {
+    const int k = k0 + (int)threadIdx.x;
     typename Piece<T, P>::V v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) v[u] = *(const typename Piece<T, P>::V*)(row + from + (k + u * NT) * P);
     float x[U * P];
     int first[U];
+    const int skip[U] = {};
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       first[u] = from + (k + u * NT) * P;
 #pragma unroll
       for (int i = 0; i < P; ++i) x[u * P + i] = (float)v[u][i];
     }
-    four(x, first);
+    f(x, first, skip, std::false_type{});
   }
-  for (; k - (int)threadIdx.x < pieces; k += NT) {
-    float x[P];
-    const int first = from + min(k, pieces - 1) * P;
-    load_piece<P, T>(row + first, x);
-    if (k >= pieces) {
-#pragma unroll
-      for (int i = 0; i < P; ++i) x[i] = -INFINITY;
-    }
-    one(x, first, k < pieces);
-  }
-  const int rest = from + pieces * P + (int)threadIdx.x;
-  if ((to - from) % P) {
-    float x[1] = {rest < to ? (float)row[rest] : -INFINITY};
-    one(x, rest, rest < to);
-  }
+  const int k = k0 + (int)threadIdx.x, left = pieces - k0;
+  if (left > 3 * NT) last_step<4, NT>(row, from, to, k, f);
+  else if (left > 2 * NT) last_step<3, NT>(row, from, to, k, f);
+  else if (left > NT) last_step<2, NT>(row, from, to, k, f);
+  else if (left > 0) last_step<1, NT>(row, from, to, k, f);
 }
 
 template <int N>
@@ -387,31 +598,28 @@ __device__ __forceinline__ float largest(const float (&x)[N]) {
   return most;
 }
 
-template <bool ENT, bool TOP, int NT, class T>
-__device__ __forceinline__ Sums row_sums(const T* __restrict__ row, int from, int to, float c, TopList& top) {
+template <int N>
+__device__ __forceinline__ bool any_nan(const float (&x)[N]) {
+  bool is = false;
+#pragma unroll
+  for (int i = 0; i < N; ++i) is |= x[i] != x[i];
+  return is;
+}
+
+template <bool ENT, int NT, class T, class LIST>
+__device__ __forceinline__ Sums row_sums(const T* __restrict__ row, int from, int to, float c, LIST& top) {
   Sums s{kLowest, 0.f, 0.f};
-  sweep<NT>(
-      row, from, to,
-      [&](const auto& x, const auto& first) {
-        constexpr int N = sizeof(x) / sizeof(float), U = sizeof(first) / sizeof(int), P = N / U;
-        const float most = largest(x);
-        add_values<ENT>(s, x, most, c);
-        if constexpr (TOP) {
-          if (!__any(!(most < top.least_value) || s.sum != s.sum)) return;
-#pragma unroll
-          for (int i = 0; i < N; ++i)
-            if (__any(!(x[i] < top.least_value))) top.put(key_of(x[i], first[i / P] + i % P));
-        }
-      },
-      [&](const auto& x, int first, bool there) {
-        constexpr int N = sizeof(x) / sizeof(float);
-        add_values<ENT>(s, x, largest(x), c);
-        if constexpr (TOP) {
-#pragma unroll
-          for (int i = 0; i < N; ++i)
-            if (__any(there && !(x[i] < top.least_value))) top.put(there ? key_of(x[i], first + i) : 0);
-        }
-      });
+  sweep<NT>(row, from, to, [&](const auto& x, const auto& first, const auto& skip, auto edge) {
+    constexpr int N = sizeof(x) / sizeof(float), P = N / (sizeof(first) / sizeof(int));
+    constexpr bool kEdge = decltype(edge)::value;
+    const float most = largest(x);
+    add_values<ENT>(s, x, most, c);
+    if constexpr (!std::is_same_v<LIST, NoList>) {  // a sum with NaN stays one: the largest does not tell of it
+      const bool nan = __any(s.sum != s.sum) && any_nan(x);
+      top.offer(x, most, nan, !kEdge || skip[0] < P, [&](int i) { return !kEdge || i % P >= skip[i / P]; },
+                [&](int i) { return min(first[0] + i / P * NT * P, to - P) + i % P; });
+    }
+  });
   return s;
 }
 
@@ -419,7 +627,7 @@ __device__ __forceinline__ Sums row_sums(const T* __restrict__ row, int from, in
 template <class T, int NT, bool ENT, bool TOP>
 __global__ __launch_bounds__(NT) void k_token_wide(TokenRows t, TokenOut o, int splits, int per, TokenParts parts) {
   __shared__ Sums part[NT / kWave];
-  __shared__ Key lists[TOP ? NT : 1];
+  __shared__ std::conditional_t<TOP, TopRoom<NT>, NoList> room;
   const T* x = (const T*)t.logits;
   const int64_t work = t.rows * splits;
   for (int64_t b = blockIdx.x; b < work; b += gridDim.x) {
@@ -434,50 +642,88 @@ __global__ __launch_bounds__(NT) void k_token_wide(TokenRows t, TokenOut o, int 
       continue;
     }
     const float at = (float)x[row * t.ld + token];
-    TopList top(TOP ? o.top : 1);
     const int from = split * per;
-    Sums s = row_sums<ENT, TOP, NT>(x + row * t.ld, from, min(t.cols, from + per), t.c, top);
+    Sums s;
+    Key list = 0;
+    if constexpr (TOP) {
+      TopList<NT> top(o.top, &room);
+      s = row_sums<ENT, NT>(x + row * t.ld, from, min(t.cols, from + per), t.c, top);
+      list = top.finish();
+    } else {
+      NoList none;
+      s = row_sums<ENT, NT>(x + row * t.ld, from, min(t.cols, from + per), t.c, none);
+    }
     join_block<ENT, NT>(s, t.c, part);
-    if constexpr (TOP) join_lists<NT / kWave>(top.list, lists);
     if (splits > 1) {
       if (threadIdx.x == 0) parts.sums[b] = f4{s.most, s.sum, s.tilt, 0.f};
-      if (TOP && threadIdx.x < kWave) parts.lists[b * kWave + threadIdx.x] = top.list;
+      if (TOP && threadIdx.x < kWave) parts.lists[b * kWave + threadIdx.x] = list;
     } else {
-      if (threadIdx.x == 0) put_numbers(o, t, row, s, token, at);
-      if (TOP && threadIdx.x < kWave) put_top(o, t, row, s, top.list, threadIdx.x);
+      if (threadIdx.x == 0) put_numbers(o, t, row, s, at);
+      if (TOP && threadIdx.x < kWave) put_top(o, t, row, s, list, threadIdx.x);
     }
     __syncthreads();
   }
 }
 
-// The parts of a row joined by a block.
-constexpr int kJoinThreads = 256;
+// The parts of a row joined by a block.  Of the lists the keys that are no smaller than the last one of some list; a wavefront
+// has those of splits w, w + 16, ...
 template <class T, bool TOP>
-__global__ __launch_bounds__(kJoinThreads) void k_token_join(TokenRows t, TokenOut o, int splits, TokenParts parts) {
-  __shared__ Key lists[TOP ? kJoinThreads : 1];
+__global__ __launch_bounds__(TOP ? 1024 : kWave) void k_token_join(TokenRows t, TokenOut o, int splits, TokenParts parts) {
+  constexpr int W = TOP ? 16 : 1, M = kWave / W;
+  __shared__ Key keys[TOP ? kWave * kWave : 1];
+  __shared__ int counts[W];
   const int lane = threadIdx.x % kWave, w = threadIdx.x / kWave;
   const int64_t row = blockIdx.x;
   const int64_t token = t.tokens ? t.tokens[row] : 0;
-  const bool counts = (uint64_t)token < (uint64_t)t.cols;
-  if (!counts) {
+  const f4 p = parts.sums[row * splits + min(lane, splits - 1)];
+  Key mine[M], least = 0;
+  if constexpr (TOP) {
+    const Key* lists = parts.lists + row * splits * kWave;
+#pragma unroll
+    for (int k = 0; k < M; ++k) mine[k] = lists[min(k * W + w, splits - 1) * kWave + lane];
+    least = lists[min(lane, splits - 1) * kWave + o.top - 1];
+  }
+  if ((uint64_t)token >= (uint64_t)t.cols) {
     if (threadIdx.x == 0) put_none(o, t, row);
     if (TOP && w == 0) put_top(o, t, row, Sums{0.f, 0.f, 0.f}, 0, lane);
     return;
   }
   const float at = (float)((const T*)t.logits)[row * t.ld + token];
   Sums s{kLowest, 0.f, 0.f};
-  if (lane < splits) {
-    const f4 p = parts.sums[row * splits + lane];
-    s = Sums{p.x, p.y, p.z};
-  }
+  if (lane < splits) s = Sums{p.x, p.y, p.z};
   join_lanes<true, kWave>(s, t.c);
-  if (threadIdx.x == 0) put_numbers(o, t, row, s, token, at);
+  if (threadIdx.x == 0) put_numbers(o, t, row, s, at);
   if constexpr (TOP) {
-    Key list = 0;
-    for (int k = w; k < splits; k += kJoinThreads / kWave)
-      list = joined(list, parts.lists[(row * splits + k) * kWave + lane]);
-    join_lists<kJoinThreads / kWave>(list, lists);
-    if (w == 0) put_top(o, t, row, s, list, lane);
+    least = max_key(least, across<1>(least));
+    least = max_key(least, across<2>(least));
+    least = max_key(least, across<4>(least));
+    least = max_key(least, across<8>(least));
+    least = max_key(least, across<16>(least));
+    least = max_key(least, across<32>(least));
+    uint64_t mask[M];
+    int n = 0;
+#pragma unroll
+    for (int k = 0; k < M; ++k) {
+      mask[k] = __ballot(k * W + w < splits && lane < o.top && mine[k] >= least && mine[k] != 0);
+      n += __popcll(mask[k]);
+    }
+    if (lane == 0) counts[w] = n;
+    __syncthreads();
+    const int before = counts[lane % W];
+    int from = 0, all = 0;
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+      const int c = __builtin_amdgcn_readlane(before, k);
+      from += k < w ? c : 0;
+      all += c;
+    }
+#pragma unroll
+    for (int k = 0; k < M; ++k) {
+      if (mask[k] >> lane & 1) keys[from + lane_place(mask[k])] = mine[k];
+      from += __popcll(mask[k]);
+    }
+    __syncthreads();
+    if (w == 0) put_top(o, t, row, s, listed(keys, all), lane);
   }
 }
 
@@ -547,8 +793,8 @@ __global__ __launch_bounds__(NT) void k_token_loss(TokenRows t, const float* __r
       if (threadIdx.x == 0) logprob[row] = 0.f;
     } else {
       const float at = (float)x[token];
-      TopList none(1);
-      Sums s = row_sums<false, false, NT>(x, 0, t.cols, t.c, none);
+      NoList none;
+      Sums s = row_sums<false, NT>(x, 0, t.cols, t.c, none);
       join_block<false, NT>(s, t.c, part);  // its barrier also stands between all reads of x[token] and the first write
       g = loss_gradient(t, s, weights ? weight * weights[row] : weight, token);
       if (threadIdx.x == 0) logprob[row] = s.sum == 0.f ? -INFINITY : (at - s.most) * t.scale - log_sum(s);
@@ -566,20 +812,21 @@ static int grid_of(int64_t blocks) { return (int)std::min(blocks, kMostBlocks); 
 
 // Lanes and pieces of narrow rows: f(L, N) as constants; false: wider ones.
 template <class T, class F>
-static bool with_narrow(int cols, bool few, F&& f) {
+static bool with_narrow(int cols, bool list, F&& f) {
   constexpr int P = 16 / sizeof(T);
   if (cols <= 4 * P) f(std::integral_constant<int, 4>{}, std::integral_constant<int, 1>{});
-  else if (cols <= 16 * P) f(std::integral_constant<int, 16>{}, std::integral_constant<int, 1>{});
-  else if (cols <= 64 * P) f(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{});
-  else if (!few && cols <= 256 * P) f(std::integral_constant<int, 64>{}, std::integral_constant<int, 4>{});
+  else if (cols <= 8 * P) f(std::integral_constant<int, 4>{}, std::integral_constant<int, 2>{});
+  else if (cols <= 16 * P) f(std::integral_constant<int, 4>{}, std::integral_constant<int, 4>{});
+  else if (cols <= 64 * P) f(std::integral_constant<int, 16>{}, std::integral_constant<int, 4>{});
+  else if (!list && cols <= 256 * P) f(std::integral_constant<int, 64>{}, std::integral_constant<int, 4>{});
   else return false;
   return true;
 }
 
 // How many blocks take a row of few rows, and how many columns each.
-static int splits_of(int64_t rows, int cols, int* per) {
+static int splits_of(int64_t rows, int cols, int step, int* per) {
   int64_t n = std::min<int64_t>(kTokenParts / std::max<int64_t>(rows, 1), kWave);
-  n = std::max<int64_t>(1, std::min<int64_t>(n, cols / 4096));
+  n = std::max<int64_t>(1, std::min<int64_t>(n, (cols + step / 2) / step));
   *per = (int)((cols + n - 1) / n + 7) / 8 * 8;
   return (cols + *per - 1) / *per;
 }
@@ -595,18 +842,18 @@ void launch_token_scores(const TokenRows& t, int type, const TokenOut& o, const 
   with_type(type, [&](auto ti) {
     typedef decltype(ti) T;
     const bool narrow = with_narrow<T>(t.cols, o.top_ids != nullptr, [&](auto l, auto n) {
-      constexpr int L = decltype(l)::value, N = decltype(n)::value, kSide = kNarrowThreads / L;
+      constexpr int L = decltype(l)::value, N = decltype(n)::value, kSide = kNarrowThreads / L * kNarrowRows<N>;
       k_token_narrow<T, L, N><<<grid_of((t.rows + kSide - 1) / kSide), kNarrowThreads, 0, st>>>(t, o);
     });
     if (narrow) return;
     int per;
-    const int splits = splits_of(t.rows, t.cols, &per);
-    constexpr int NT = 512;
+    constexpr int NT = 256;
+    const int splits = splits_of(t.rows, t.cols, NT * 64 / (int)sizeof(T), &per);
     if (o.entropy) launch_wide<T, NT, true>(t, o, splits, per, parts, st);
     else launch_wide<T, NT, false>(t, o, splits, per, parts, st);
     if (splits == 1) return;
-    if (o.top_ids) k_token_join<T, true><<<(int)t.rows, kJoinThreads, 0, st>>>(t, o, splits, parts);
-    else k_token_join<T, false><<<(int)t.rows, kJoinThreads, 0, st>>>(t, o, splits, parts);
+    if (o.top_ids) k_token_join<T, true><<<(int)t.rows, 1024, 0, st>>>(t, o, splits, parts);
+    else k_token_join<T, false><<<(int)t.rows, kWave, 0, st>>>(t, o, splits, parts);
   });
 }
 
@@ -644,7 +891,7 @@ void launch_token_loss(const TokenRows& t, int type, const float* weights, float
       typedef decltype(tout) TO;
       TO* to = (TO*)dx.data;
       const bool narrow = with_narrow<T>(t.cols, false, [&](auto l, auto n) {
-        constexpr int L = decltype(l)::value, N = decltype(n)::value, kSide = kNarrowThreads / L;
+        constexpr int L = decltype(l)::value, N = decltype(n)::value, kSide = kNarrowThreads / L * kNarrowRows<N>;
         k_token_loss_narrow<T, TO, L, N><<<grid_of((t.rows + kSide - 1) / kSide), kNarrowThreads, 0, st>>>(
             t, weights, weight, logprob, to, dx.ld);
       });
