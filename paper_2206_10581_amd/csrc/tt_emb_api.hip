@@ -103,7 +103,7 @@ void launch_bias(const tt_emb_matrix& table, const tt_emb_distances&, float fill
                  const tt_emb_pairs& out, hipStream_t);
 SumPlan sum_plan(const tt_emb_pairs&, int span, bool offsets);
 void launch_bias_sums(const tt_emb_pairs&, const tt_emb_distances&, const tt_emb_matrix& out, bool add, const SumPlan&,
-                      double* total, float* parts, hipStream_t);
+                      double* total, PartReach* reach, float* parts, hipStream_t);
 hipError_t calibrate(void* buf, size_t bytes, hipStream_t, double* copy_bytes_per_s,
                      double* mfma_flops_per_s, double* gather_bytes_per_s,
                      double* far_gather_bytes_per_s);
@@ -1452,18 +1452,32 @@ int tt_emb_bias_forward(const tt_emb_matrix* table, const tt_emb_distances* dist
   return e == hipSuccess ? TT_EMB_OK : hip_fail(e);
 }
 
-// The totals of all distances and heads, and then the parts.
-static size_t total_bytes(const tt_emb_pairs& g, const SumPlan& p, int span) {
-  return p.parts == 0 ? 0 : ((size_t)(2 * (int64_t)span + 1) * g.heads * sizeof(double) + 255) & ~(size_t)255;
-}
-static size_t sums_bytes(const tt_emb_pairs& g, const SumPlan& p, int span) {
-  return total_bytes(g, p, span) + (((size_t)(p.parts * p.width) * sizeof(float) + 255) & ~(size_t)255);
+// The totals of all distances and heads, what the parts reach, and the parts.
+struct SumWork {
+  double* total;
+  PartReach* reach;
+  float* parts;
+};
+static size_t carve_sums(const tt_emb_pairs& g, const SumPlan& p, int span, char* base, SumWork* ws) {
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    char* at = base + off;
+    off += (bytes + 255) & ~(size_t)255;
+    return at;
+  };
+  if (p.parts == 0) return 0;
+  SumWork w{};
+  w.total = (double*)take((size_t)(2 * (int64_t)span + 1) * g.heads * sizeof(double));
+  w.reach = (PartReach*)take((size_t)p.parts * sizeof(PartReach));
+  w.parts = (float*)take((size_t)(p.parts * p.width) * sizeof(float));
+  if (ws != nullptr) *ws = w;
+  return off;
 }
 
 int tt_emb_bias_workspace_bytes(const tt_emb_pairs* grad, int32_t span, size_t* bytes) {
   if (bytes == nullptr || !good_sizes(grad) || span < 0 || span > 1 << 20) return TT_EMB_EINVAL;
-  *bytes = std::max(sums_bytes(*grad, sum_plan(*grad, span, false), span),
-                    sums_bytes(*grad, sum_plan(*grad, span, true), span));
+  *bytes = std::max(carve_sums(*grad, sum_plan(*grad, span, false), span, nullptr, nullptr),
+                    carve_sums(*grad, sum_plan(*grad, span, true), span, nullptr, nullptr));
   return TT_EMB_OK;
 }
 
@@ -1473,14 +1487,14 @@ int tt_emb_bias_backward(const tt_emb_pairs* grad, const tt_emb_distances* dista
       grad->heads != dtable->cols)
     return TT_EMB_EINVAL;
   const SumPlan plan = sum_plan(*grad, distances->span, distances->offsets != nullptr);
-  const size_t needed = sums_bytes(*grad, plan, distances->span);
+  SumWork ws{};
+  const size_t needed = carve_sums(*grad, plan, distances->span, (char*)workspace, &ws);
   if (needed > 0) {
     const int rc = check_workspace(workspace, workspace_bytes, needed);
     if (rc != TT_EMB_OK) return rc;
   }
   if (dtable->rows == 0) return TT_EMB_OK;
-  float* parts = (float*)((char*)workspace + total_bytes(*grad, plan, distances->span));
-  launch_bias_sums(*grad, *distances, *dtable, add != 0, plan, (double*)workspace, parts, (hipStream_t)hip_stream);
+  launch_bias_sums(*grad, *distances, *dtable, add != 0, plan, ws.total, ws.reach, ws.parts, (hipStream_t)hip_stream);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? TT_EMB_OK : hip_fail(e);
 }

@@ -27,46 +27,124 @@ __device__ __forceinline__ float any_value(const tt_emb_matrix& m, int64_t at) {
   return ((const float*)m.data)[at];
 }
 
-// ---- bias of tiles
+// a / b for a >= 0, b > 0: in 64 bits a division takes a microsecond
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+  return (uint64_t)(a | b) >> 32 ? a / b : (int64_t)((uint32_t)a / (uint32_t)b);
+}
+
+// ---- bias
+
+// The bias of distances in one head.
+struct Values {
+  tt_emb_matrix table;
+  const int32_t* bucket_of;
+  int span, h;
+  float fill;
+  __device__ __forceinline__ int bucket(int64_t distance) const { return bucket_of[cut(distance, span) + span]; }
+  __device__ __forceinline__ float of(int u) const {
+    return (uint32_t)u < (uint32_t)table.rows ? any_value(table, u * table.ld + h) : fill;
+  }
+  // Of N distances, `step` apart, all buckets before all values.
+  template <int N>
+  __device__ __forceinline__ void get(int64_t first, int step, float (&v)[N]) const {
+    int u[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) u[i] = bucket(first + i * step);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = of(u[i]);
+  }
+};
+__device__ __forceinline__ float added(float x, float bias) { return isinf(bias) ? bias : x + bias; }
 
 constexpr int kBiasThreads = 256, kBiasAhead = 4;  // rows of a tile that a thread has under way
+template <class TI, class TO, bool ADD>
+constexpr int kBiasPiece = 16 / (ADD && sizeof(TI) > sizeof(TO) ? sizeof(TI) : sizeof(TO));
+
+// Few queries: a block takes a row, a thread looks up its pieces' values; those beyond the span have one for all.
+constexpr int kFewQueries = 4;
+template <class TI, class TO, bool ADD>
+__global__ __launch_bounds__(kBiasThreads) void k_bias_few(tt_emb_matrix table, tt_emb_distances dist, float fill,
+                                                           tt_emb_pairs in, tt_emb_pairs out, int64_t count) {
+  constexpr int P = kBiasPiece<TI, TO, ADD>;
+  for (int64_t row = blockIdx.x; row < count; row += gridDim.x) {
+    const int64_t plane = quotient(row, out.queries);
+    const int i = (int)(row - plane * out.queries), b = (int)quotient(plane, out.heads), h = (int)(plane - (int64_t)b * out.heads);
+    const int64_t first = offset_of(dist, b) - i;  // distance of the first key
+    const Values values{table, dist.bucket_of, dist.span, h, fill};
+    const float low = values.of(values.bucket(-dist.span)), high = values.of(values.bucket(dist.span));
+    const TI* from = (const TI*)in.data + (ADD ? b * in.batch_ld + h * in.head_ld + i * in.query_ld : 0);
+    TO* to = (TO*)out.data + b * out.batch_ld + h * out.head_ld + i * out.query_ld;
+    const int keys = (int)out.keys;
+    for (int c = (int)threadIdx.x * P; c < keys; c += kBiasThreads * P) {
+      if (c + P > keys) {  // cut off
+        for (int j = c; j < keys; ++j) {
+          float y = values.of(values.bucket(first + j));
+          if constexpr (ADD) y = added((float)from[j], y);
+          to[j] = (TO)y;
+        }
+        continue;
+      }
+      float x[P], y[P];
+      if constexpr (ADD) load_piece<P, TI>(from + c, x);
+      const bool before = first + c + P - 1 <= -dist.span, behind = first + c >= dist.span;
+      if (before || behind) {
+#pragma unroll
+        for (int k = 0; k < P; ++k) y[k] = before ? low : high;
+      } else {
+        values.get(first + c, 1, y);
+      }
+      if constexpr (ADD) {
+#pragma unroll
+        for (int k = 0; k < P; ++k) y[k] = added(x[k], y[k]);
+      }
+      store_piece<P, TO, ADD>(to + c, y);
+    }
+  }
+}
+
 struct BiasTiles {
   int rows, cols;  // of a tile
   int down, across;
   int64_t count;
   int lanes;       // log2 of the threads side by side
-  int line;        // places of a line: rows + cols and some more, a multiple of 4
+  int line;        // places of a line: rows + cols and some more, a multiple of 8
 };
 
 // A block takes a tile of one head.  Its diagonals' values come first, four copies of the line, each a place further, so that
-// any row finds its values in 16-byte words of one of them; a tile beyond the span has one value.
+// any row finds its values in 16-byte words of one of them; a tile beyond the span has one value.  Where a thread takes two
+// words of them, those of even and odd number lie apart, so that the threads of a wavefront read side by side.
 template <class TI, class TO, bool ADD>
 __global__ __launch_bounds__(kBiasThreads) void k_bias_tiles(tt_emb_matrix table, tt_emb_distances dist, float fill,
                                                              tt_emb_pairs in, tt_emb_pairs out, BiasTiles tl) {
   extern __shared__ __attribute__((aligned(16))) float lines[];
-  constexpr int P = 16 / (ADD && sizeof(TI) > sizeof(TO) ? sizeof(TI) : sizeof(TO)), R = kBiasAhead;
+  constexpr int P = kBiasPiece<TI, TO, ADD>, R = kBiasAhead, kAhead = 4;
   const int side = threadIdx.x & ((1 << tl.lanes) - 1), up = threadIdx.x >> tl.lanes, step = kBiasThreads >> tl.lanes;
+  auto word = [&](int copy, int w) {  // where the word's four values are
+    return copy * tl.line + (P == 8 ? (w & 1) * (tl.line / 2) + w / 2 * 4 : w * 4);
+  };
   for (int64_t tile = blockIdx.x; tile < tl.count; tile += gridDim.x) {
-    const int64_t plane = tile / ((int64_t)tl.down * tl.across);
-    const int64_t place = tile - plane * tl.down * tl.across;
-    const int b = (int)(plane / out.heads), h = (int)(plane - (int64_t)b * out.heads);
-    const int i0 = (int)(place / tl.across) * tl.rows, j0 = (int)(place % tl.across) * tl.cols;
+    const int64_t strip = quotient(tile, tl.across), plane = quotient(strip, tl.down);
+    const int j0 = (int)(tile - strip * tl.across) * tl.cols, i0 = (int)(strip - plane * tl.down) * tl.rows;
+    const int b = (int)quotient(plane, out.heads), h = (int)(plane - (int64_t)b * out.heads);
     const int rows = (int)min((int64_t)tl.rows, out.queries - i0), cols = (int)min((int64_t)tl.cols, out.keys - j0);
     const int64_t first = offset_of(dist, b) + j0 - i0 - (rows - 1);  // distance of the first diagonal
-    auto value = [&](int64_t distance) {
-      const int u = dist.bucket_of[cut(distance, dist.span) + dist.span];
-      return (uint32_t)u < (uint32_t)table.rows ? any_value(table, u * table.ld + h) : fill;
-    };
+    const Values values{table, dist.bucket_of, dist.span, h, fill};
     const bool one = first >= dist.span || first + rows + cols - 2 <= -dist.span;
     float all = 0.f;
     if (one) {
-      all = value(first);
+      all = values.of(values.bucket(first));
     } else {
-      for (int x = threadIdx.x; x < rows + cols - 1; x += kBiasThreads) {
-        const float v = value(first + x);
+      for (int x0 = threadIdx.x; x0 < rows + cols - 1; x0 += kAhead * kBiasThreads) {
+        float v[kAhead];
+        values.get(first + x0, kBiasThreads, v);
 #pragma unroll
-        for (int s = 0; s < 4; ++s)
-          if (x >= s) lines[s * tl.line + x - s] = v;
+        for (int k = 0; k < kAhead; ++k) {
+          const int x = x0 + k * kBiasThreads;
+          if (x >= rows + cols - 1) continue;
+#pragma unroll
+          for (int s = 0; s < 4; ++s)
+            if (x >= s) lines[word(s, (x - s) / 4) + (x - s) % 4] = v[k];
+        }
       }
       __syncthreads();
     }
@@ -77,8 +155,9 @@ __global__ __launch_bounds__(kBiasThreads) void k_bias_tiles(tt_emb_matrix table
         if (c + P > cols) {  // cut off
           for (int r = r0; r < rows && r < r0 + step * R; r += step)
             for (int i = c; i < cols; ++i) {
-              float y = one ? all : lines[i - r + rows - 1];
-              if constexpr (ADD) y = isinf(y) ? y : (float)from[r * in.query_ld + i] + y;
+              const int a = i - r + rows - 1;
+              float y = one ? all : lines[word(0, a / 4) + a % 4];
+              if constexpr (ADD) y = added((float)from[r * in.query_ld + i], y);
               to[r * out.query_ld + i] = (TO)y;
             }
           continue;
@@ -98,17 +177,17 @@ __global__ __launch_bounds__(kBiasThreads) void k_bias_tiles(tt_emb_matrix table
 #pragma unroll
             for (int i = 0; i < P; ++i) y[i] = all;
           } else {
-            const int a = c - r + rows - 1, s = a & 3;
+            const int a = c - r + rows - 1;
 #pragma unroll
             for (int i = 0; i < P; i += 4) {
-              const f4 w = *(const f4*)&lines[s * tl.line + a - s + i];
+              const f4 w = *(const f4*)&lines[word(a % 4, a / 4 + i / 4)];
 #pragma unroll
               for (int n = 0; n < 4; ++n) y[i + n] = w[n];
             }
           }
           if constexpr (ADD) {
 #pragma unroll
-            for (int i = 0; i < P; ++i) y[i] = isinf(y[i]) ? y[i] : (float)v[k][i] + y[i];
+            for (int i = 0; i < P; ++i) y[i] = added((float)v[k][i], y[i]);
           }
           store_piece<P, TO, ADD>(to + r * out.query_ld + c, y);
         }
@@ -151,7 +230,7 @@ struct Extent {
 // diagonal are summed apart, row by row.
 template <class T, int B>
 __global__ __launch_bounds__(kSumThreads) void k_bias_sums(tt_emb_pairs g, tt_emb_distances dist, int buckets, SumPlan p,
-                                                           float* __restrict__ parts) {
+                                                           float* __restrict__ parts, PartReach* __restrict__ reach) {
   typedef typename Piece<T, 16 / sizeof(T)>::V VF;
   typedef typename Piece<T, B>::V VB;
   constexpr int P = 16 / sizeof(T), R = kSumAhead;
@@ -159,9 +238,9 @@ __global__ __launch_bounds__(kSumThreads) void k_bias_sums(tt_emb_pairs g, tt_em
   const int lane = threadIdx.x % kWave, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
   const Extent<T> all(g);
   for (int64_t part = blockIdx.x; part < p.parts; part += gridDim.x) {
-    const int64_t plane = part / p.chunks;
+    const int64_t plane = quotient(part, p.chunks);
     const int chunk = (int)(part - plane * p.chunks);
-    const int h = (int)(plane / p.groups), b0 = (int)(plane - (int64_t)h * p.groups) * p.group;
+    const int h = (int)quotient(plane, p.groups), b0 = (int)(plane - (int64_t)h * p.groups) * p.group;
     const int b1 = min(b0 + p.group, g.batch), i0 = chunk * p.rows, i1 = (int)min((int64_t)i0 + p.rows, g.queries);
     const int keys = (int)g.keys;
     const int64_t offset = offset_of(dist, b0);
@@ -244,8 +323,10 @@ __global__ __launch_bounds__(kSumThreads) void k_bias_sums(tt_emb_pairs g, tt_em
     }
     __syncthreads();
     // what lies between, as far as these rows reach
-    const int end = min(d.last, keys - i0);
-    for (int x0 = max(d.first + 1, 1 - i1); x0 < end; x0 += kWave * B) {
+    const int start = max(d.first + 1, 1 - i1), end = min(d.last, keys - i0);
+    if (threadIdx.x == 0)
+      reach[part] = PartReach{cut(d.first + offset, dist.span), cut(d.last + offset, dist.span), start - d.first, end - d.first};
+    for (int x0 = start; x0 < end; x0 += kWave * B) {
       const int x = x0 + lane * B;  // this lane's first diagonal; what it sums beyond the end is left
       float acc[B] = {};
       for (int b = b0; b < b1; ++b) {
@@ -299,37 +380,29 @@ __global__ __launch_bounds__(kSumThreads) void k_bias_sums(tt_emb_pairs g, tt_em
 }
 
 // total[distance][head]: all parts of a head and distance, in fp64.  A block has 64 distances, a wavefront every 16th part.
-constexpr int kJoinThreads = 1024, kJoinWaves = kJoinThreads / kWave, kJoinAhead = 4;
-__global__ __launch_bounds__(kJoinThreads) void k_bias_join(tt_emb_pairs g, tt_emb_distances dist, SumPlan p,
-                                                            const float* __restrict__ parts, double* __restrict__ total) {
+constexpr int kJoinThreads = 1024, kJoinWaves = kJoinThreads / kWave, kJoinAhead = 8;
+__global__ __launch_bounds__(kJoinThreads) void k_bias_join(int heads, int span, SumPlan p, const float* __restrict__ parts,
+                                                            const PartReach* __restrict__ reach, double* __restrict__ total) {
   __shared__ double sums[kJoinWaves][kWave];
   const int lane = threadIdx.x % kWave, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
-  const int per_head = p.groups * p.chunks, distances = 2 * dist.span + 1;
-  const int64_t tiles = (distances + kWave - 1) / kWave;
-  for (int64_t tile = blockIdx.x; tile < tiles * g.heads; tile += gridDim.x) {
-    const int h = (int)(tile / tiles), r = (int)(tile - h * tiles) * kWave + lane, distance = r - dist.span;
+  const int per_head = p.groups * p.chunks, distances = 2 * span + 1, tiles = (distances + kWave - 1) / kWave;
+  for (int64_t tile = blockIdx.x; tile < (int64_t)tiles * heads; tile += gridDim.x) {
+    const int h = (int)quotient(tile, tiles), r = (int)(tile - (int64_t)h * tiles) * kWave + lane, distance = r - span;
     double sum = 0.0;
     for (int k0 = w; k0 < per_head; k0 += kJoinWaves * kJoinAhead) {
+      PartReach a[kJoinAhead];
       float v[kJoinAhead];
-      bool is[kJoinAhead];
+#pragma unroll
+      for (int n = 0; n < kJoinAhead; ++n) a[n] = reach[(int64_t)h * per_head + min(k0 + n * kJoinWaves, per_head - 1)];
 #pragma unroll
       for (int n = 0; n < kJoinAhead; ++n) {
-        const int k = min(k0 + n * kJoinWaves, per_head - 1), group = k / p.chunks, chunk = k - group * p.chunks;
-        const int64_t offset = offset_of(dist, group * p.group);
-        const Span d = span_of(g, offset, dist.span);
-        // the diagonal of this distance; the ends stand for more than their own
-        int64_t diagonal = distance - offset;
-        const bool end = (distance == -dist.span && d.first + offset <= distance) ||
-                         (distance == dist.span && d.last + offset >= distance);
-        if (end) diagonal = distance == -dist.span && d.first + offset <= distance ? d.first : d.last;
-        // what the part's rows do not reach is not written
-        const int64_t i0 = (int64_t)chunk * p.rows, i1 = min(i0 + p.rows, g.queries);
-        is[n] = k0 + n * kJoinWaves < per_head && r < distances && diagonal >= d.first && diagonal <= d.last &&
-                (diagonal == d.first || diagonal == d.last || (diagonal > -i1 && diagonal < g.keys - i0));
-        v[n] = is[n] ? parts[((int64_t)h * per_head + k) * p.width + (diagonal - d.first)] : 0.f;
+        const int k = k0 + n * kJoinWaves, at = distance - a[n].first, last = a[n].last - a[n].first;
+        v[n] = 0.f;
+        if (k < per_head && r < distances && (at == 0 || at == last || (at > 0 && at < last && at >= a[n].start && at < a[n].end)))
+          v[n] = parts[((int64_t)h * per_head + k) * p.width + at];
       }
 #pragma unroll
-      for (int n = 0; n < kJoinAhead; ++n) sum += is[n] ? (double)v[n] : 0.0;
+      for (int n = 0; n < kJoinAhead; ++n) sum += (double)v[n];
     }
     sums[w][lane] = sum;
     __syncthreads();
@@ -337,7 +410,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_bias_join(tt_emb_pairs g, tt_e
       sum = 0.0;
 #pragma unroll
       for (int k = 0; k < kJoinWaves; ++k) sum += sums[k][lane];
-      total[(int64_t)r * g.heads + h] = sum;
+      total[(int64_t)r * heads + h] = sum;
     }
     __syncthreads();
   }
@@ -389,31 +462,37 @@ __global__ __launch_bounds__(kSumThreads) void k_bias_buckets(int heads, tt_emb_
 
 constexpr int64_t kMostBlocks = 1 << 20;
 
-void launch_bias(const tt_emb_matrix& table, const tt_emb_distances& dist, float fill, const tt_emb_pairs* in,
-                 const tt_emb_pairs& out, hipStream_t st) {
-  BiasTiles tl;
-  const int size = std::max(type_size(out.type), in ? type_size(in->type) : 0), P = 16 / size;
+template <class TI, class TO, bool ADD>
+static void launch_bias_of(const tt_emb_matrix& table, const tt_emb_distances& dist, float fill, const tt_emb_pairs& in,
+                           const tt_emb_pairs& out, hipStream_t st) {
+  constexpr int P = kBiasPiece<TI, TO, ADD>;
   const int64_t planes = (int64_t)out.batch * out.heads;
-  tl.cols = (int)std::min<int64_t>((out.keys + P - 1) / P * P, out.queries <= 8 ? 2048 : 1024);
+  if (out.queries <= kFewQueries) {
+    const int64_t rows = planes * out.queries;
+    k_bias_few<TI, TO, ADD><<<(int)std::min(rows, kMostBlocks), kBiasThreads, 0, st>>>(table, dist, fill, in, out, rows);
+    return;
+  }
+  BiasTiles tl;
+  tl.cols = (int)std::min<int64_t>((out.keys + P - 1) / P * P, kBiasThreads * P);
   tl.across = (int)((out.keys + tl.cols - 1) / tl.cols);
-  tl.rows = (int)std::min<int64_t>(std::min<int64_t>(out.queries, 1088 - std::min(tl.cols, 1024)), 65536 / tl.cols);
+  tl.rows = (int)std::min<int64_t>(out.queries, std::min(1024, 32 * kBiasThreads * P / tl.cols));
   // enough tiles for all compute units
-  while (tl.rows > 8 && planes * tl.across * ((out.queries + tl.rows - 1) / tl.rows) < 2048) tl.rows /= 2;
+  while (tl.rows > 8 && planes * tl.across * ((out.queries + tl.rows - 1) / tl.rows) < 4096) tl.rows /= 2;
   tl.down = (int)((out.queries + tl.rows - 1) / tl.rows);
   tl.count = planes * tl.down * tl.across;
   tl.lanes = 0;
   while ((1 << tl.lanes) < kBiasThreads && (P << tl.lanes) < tl.cols) ++tl.lanes;
-  tl.line = (tl.rows + tl.cols + 11) / 4 * 4;
-  const int blocks = (int)std::min(tl.count, kMostBlocks), lds = 4 * tl.line * (int)sizeof(float);
+  tl.line = (tl.rows + tl.cols + 15) / 8 * 8;
+  k_bias_tiles<TI, TO, ADD><<<(int)std::min(tl.count, kMostBlocks), kBiasThreads, 4 * tl.line * (int)sizeof(float), st>>>(
+      table, dist, fill, in, out, tl);
+}
+
+void launch_bias(const tt_emb_matrix& table, const tt_emb_distances& dist, float fill, const tt_emb_pairs* in,
+                 const tt_emb_pairs& out, hipStream_t st) {
   with_type(out.type, [&](auto to) {
     typedef decltype(to) TO;
-    if (in == nullptr) {
-      k_bias_tiles<TO, TO, false><<<blocks, kBiasThreads, lds, st>>>(table, dist, fill, out, out, tl);
-      return;
-    }
-    with_type(in->type, [&](auto ti) {
-      k_bias_tiles<decltype(ti), TO, true><<<blocks, kBiasThreads, lds, st>>>(table, dist, fill, *in, out, tl);
-    });
+    if (in == nullptr) launch_bias_of<TO, TO, false>(table, dist, fill, out, out, st);
+    else with_type(in->type, [&](auto ti) { launch_bias_of<decltype(ti), TO, true>(table, dist, fill, *in, out, st); });
   });
 }
 
@@ -435,18 +514,18 @@ SumPlan sum_plan(const tt_emb_pairs& g, int span, bool offsets) {
 }
 
 void launch_bias_sums(const tt_emb_pairs& g, const tt_emb_distances& dist, const tt_emb_matrix& out, bool add,
-                      const SumPlan& p, double* total, float* parts, hipStream_t st) {
+                      const SumPlan& p, double* total, PartReach* reach, float* parts, hipStream_t st) {
   if (p.parts > 0) {
     with_type(g.type, [&](auto t) {
       typedef decltype(t) T;
       const int blocks = (int)std::min(p.parts, kMostBlocks);
       if (p.width - 2 <= kWave * 4)
-        k_bias_sums<T, 4><<<blocks, kSumThreads, 0, st>>>(g, dist, (int)out.rows, p, parts);
+        k_bias_sums<T, 4><<<blocks, kSumThreads, 0, st>>>(g, dist, (int)out.rows, p, parts, reach);
       else
-        k_bias_sums<T, 8><<<blocks, kSumThreads, 0, st>>>(g, dist, (int)out.rows, p, parts);
+        k_bias_sums<T, 8><<<blocks, kSumThreads, 0, st>>>(g, dist, (int)out.rows, p, parts, reach);
     });
     const int64_t tiles = (2 * (int64_t)dist.span + kWave) / kWave * g.heads;
-    k_bias_join<<<(int)std::min(tiles, kMostBlocks), kJoinThreads, 0, st>>>(g, dist, p, parts, total);
+    k_bias_join<<<(int)std::min(tiles, kMostBlocks), kJoinThreads, 0, st>>>(g.heads, dist.span, p, parts, reach, total);
   }
   int lanes = 0;
   while ((1 << lanes) < kWave && (1 << lanes) < g.heads) ++lanes;

@@ -600,6 +600,10 @@ struct SumPlan {
   int group, groups, rows, chunks;
 };
 constexpr int kSumParts = 2048;  // about as many at most
+// The distances that a part's first and last value stand for; of those between, values [start, end) are there, the others zero.
+struct PartReach {
+  int first, last, start, end;
+};
 
 inline int type_size(int type) { return type == TT_EMB_FP32 ? 4 : 2; }
 
