@@ -208,7 +208,8 @@ __device__ __forceinline__ Span span_of(const tt_emb_pairs& g, int64_t offset, i
   return {(int)min(max(-(int64_t)span - offset, low), high), (int)max(min((int64_t)span - offset, high), low)};
 }
 
-constexpr int kSumThreads = 256, kSumWaves = kSumThreads / kWave, kSumAhead = 4;
+constexpr int kSumThreads = 256, kSumWaves = kSumThreads / kWave;
+constexpr int kSumAhead = 4;  // rows that a wavefront has under way
 
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll
@@ -224,6 +225,37 @@ struct Extent {
     high = low + (g.batch - 1) * g.batch_ld + (g.heads - 1) * g.head_ld + (g.queries - 1) * g.query_ld + g.keys;
   }
 };
+
+// Groups [from, to) of 64 pieces in R rows, `p` in this lane's of the first.
+template <int R, class T>
+__device__ __forceinline__ float groups_sum(const T* p, int64_t ld, int from, int to) {
+  constexpr int P = 16 / sizeof(T), U = 2;
+  typedef typename Piece<T, P>::V V;
+  float sum = 0.f;
+  auto some = [&](auto count, int q) {
+    constexpr int N = decltype(count)::value;
+    V v[N][R];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int n = 0; n < N; ++n) v[n][r] = *(const V*)(p + r * ld + (q + n) * kWave * P);
+    float s[N * R];
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        s[n * R + r] = (float)v[n][r][0];
+#pragma unroll
+        for (int k = 1; k < P; ++k) s[n * R + r] += (float)v[n][r][k];
+      }
+#pragma unroll
+    for (int n = 1; n < N * R; ++n) s[0] += s[n];
+    sum += s[0];
+  };
+  for (; from + U <= to; from += U) some(std::integral_constant<int, U>{}, from);
+  for (; from < to; ++from) some(std::integral_constant<int, 1>{}, from);
+  return sum;
+}
 
 // A block sums the diagonals of some rows of one head and of p.group sequences, a lane B of them at a time: its accumulators
 // stay, the row's place moves by a value from one row to the next.  All before the first and behind the last
@@ -251,54 +283,106 @@ __global__ __launch_bounds__(kSumThreads) void k_bias_sums(tt_emb_pairs g, tt_em
     };
     const bool low = wanted(d.first), high = wanted(d.last);
     float before = 0.f, behind = 0.f;
-    // columns [0, i + until) of row i are before, [i + since, keys) behind
-    const int until = d.first + 1, since = max(d.last, d.first + 1);
+    // what lies between, as far as these rows reach: R rows of the band of 64 B diagonals from x0 on
+    const int start = max(d.first + 1, 1 - i1), end = min(d.last, keys - i0);
+    if (threadIdx.x == 0)
+      reach[part] = PartReach{cut(d.first + offset, dist.span), cut(d.last + offset, dist.span), start - d.first, end - d.first};
+    float acc[B] = {};
+    auto add_rows = [&](const T* rows, int i, int x0) {
+      const int x = x0 + lane * B, to = (int)min((int64_t)i1, (int64_t)keys - x0);  // this lane's first diagonal
+      if (i >= to || i + R + x0 + kWave * B <= 0) return;  // the band lies outside of these rows
+      const T* at = rows + i * g.query_ld + (i + x);  // a row on is a column on
+      VB v[R];
+      if (i + x0 >= 0 && i + R - 1 + x0 + kWave * B <= keys && i + R <= to) {  // within all rows, for all lanes
+#pragma unroll
+        for (int r = 0; r < R; ++r) v[r] = *(const VB*)(at + r * (g.query_ld + 1));
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+          for (int k = 0; k < B; ++k) acc[k] += (float)v[r][k];
+        return;
+      }
+      bool cut_off = false;
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const int j = i + r + x;
+        const T* q = at + r * (g.query_ld + 1);
+        const bool some = i + r < to && j + B > 0 && j < keys, whole = some && q >= all.low && q + B <= all.high;
+        v[r] = VB{};
+        if (whole) v[r] = *(const VB*)q;
+        cut_off = cut_off || (some && !whole);
+      }
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const int j = i + r + x;
+#pragma unroll
+        for (int k = 0; k < B; ++k) acc[k] += (uint32_t)(j + k) < (uint32_t)keys ? (float)v[r][k] : 0.f;
+      }
+      if (__any(cut_off)) {  // at the memory's ends: singly
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          const int j = i + r + x;
+          const T* q = at + r * (g.query_ld + 1);
+          if (i + r >= to || (q >= all.low && q + B <= all.high)) continue;
+#pragma unroll
+          for (int k = 0; k < B; ++k)
+            if ((uint32_t)(j + k) < (uint32_t)keys) acc[k] += (float)q[k];
+        }
+      }
+    };
+    const bool one_band = end > start && end - start <= kWave * B;  // taken beside the rest, whose rows are in the caches then
+    // Columns [0, i + until) of row i are before, [i + since, keys) behind.  R rows at a time: groups of 64 pieces that are so
+    // in all of them are only added up; of the others the wanted places are, and those with none are left out.
+    const int until = d.first + 1, since = max(d.last, d.first + 1), whole = keys / (kWave * P);
     for (int b = b0; b < b1; ++b) {
       const T* rows = (const T*)g.data + b * g.batch_ld + h * g.head_ld;
       for (int i = i0 + w * R; i < i1; i += kSumWaves * R) {
-        const int n = min(R, i1 - i), most = low ? i + n - 1 + until : 0, least = high ? i + since : keys;
-        for (int c0 = 0; c0 < keys; c0 += kWave * P) {
-          if (c0 >= most && c0 + kWave * P <= least) continue;  // nothing of the group is wanted in any row
-          const int c = c0 + lane * P;
-          const T* at = rows + i * g.query_ld + c;
-          if (n == R && c0 + kWave * P <= keys && (c0 + kWave * P <= (low ? i + until : 0) || c0 >= (high ? i + R - 1 + since : keys))) {
-            VF v[R];
-#pragma unroll
-            for (int r = 0; r < R; ++r) v[r] = *(const VF*)(at + r * g.query_ld);
-            float s[R];
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-              s[r] = (float)v[r][0];
-#pragma unroll
-              for (int k = 1; k < P; ++k) s[r] += (float)v[r][k];
-            }
-            float sum = s[0];
-#pragma unroll
-            for (int r = 1; r < R; ++r) sum += s[r];
-            if (c0 < most) before += sum;
-            else behind += sum;
-            continue;
-          }
+        const T* at = rows + i * g.query_ld + lane * P;
+        const bool full = i + R <= i1;
+        const int g0 = full && low ? min(max(i + until, 0) / (kWave * P), whole) : 0;
+        const int g1 = full && high ? max(min((max(i + R - 1 + since, 0) + kWave * P - 1) / (kWave * P), whole), g0) : whole;
+        before += groups_sum<R>(at, g.query_ld, 0, g0);
+        behind += groups_sum<R>(at, g.query_ld, g1, whole);
+        for (int q = g0 < g1 ? g0 : whole; q * kWave * P < keys; q = q + 1 == g1 ? whole : q + 1) {
+          const int c0 = q * kWave * P, c = c0 + lane * P, edge = keys - c;
+          // places [0, u) of row i are before, u + 1 of the next one's
+          const int u = low ? i + until - c0 : -R, s = high ? i + since - c0 : kWave * P + R;
+          if (u + R - 1 <= 0 && s >= min(kWave * P, keys - c0)) continue;
           VF v[R];
-          bool whole[R];
 #pragma unroll
           for (int r = 0; r < R; ++r) {
-            whole[r] = r < n && c < keys && at + r * g.query_ld + P <= all.high;
-            if (whole[r]) v[r] = *(const VF*)(at + r * g.query_ld);
-          }
+            const T* p = at + r * g.query_ld + c0;
+            v[r] = VF{};
+            if (i + r >= i1 || edge <= 0) continue;
+            if (q < whole || p + P <= all.high) {
+              v[r] = *(const VF*)p;
+            } else {
 #pragma unroll
-          for (int r = 0; r < R; ++r) {
-            if (r >= n || c >= keys) continue;
-            const int u = low ? i + r + until : 0, s = high ? i + r + since : keys;
-#pragma unroll
-            for (int k = 0; k < P; ++k) {
-              if (c + k >= keys || (c + k >= u && c + k < s)) continue;
-              const float x = whole[r] ? (float)v[r][k] : (float)at[r * g.query_ld + k];
-              before += c + k < u ? x : 0.f;
-              behind += c + k < u ? 0.f : x;
+              for (int k = 0; k < P; ++k)
+                if (k < edge) v[r][k] = p[k];
             }
+          }
+          if (q >= whole) {  // the row's end: what lies behind it counts as 0
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+              for (int k = 0; k < P; ++k) v[r][k] = k < edge ? v[r][k] : (T)0.f;
+          }
+          const int lu = u - lane * P, ls = s - lane * P;
+          if (u + R - 1 > 0) {
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+              for (int k = 0; k < P; ++k) before += k - r < lu ? (float)v[r][k] : 0.f;
+          }
+          if (s < kWave * P) {
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+              for (int k = 0; k < P; ++k) behind += k - r >= ls ? (float)v[r][k] : 0.f;
           }
         }
+        if (one_band) add_rows(rows, i, start);
       }
     }
     before = wave_sum(before);
@@ -322,47 +406,15 @@ __global__ __launch_bounds__(kSumThreads) void k_bias_sums(tt_emb_pairs g, tt_em
       }
     }
     __syncthreads();
-    // what lies between, as far as these rows reach
-    const int start = max(d.first + 1, 1 - i1), end = min(d.last, keys - i0);
-    if (threadIdx.x == 0)
-      reach[part] = PartReach{cut(d.first + offset, dist.span), cut(d.last + offset, dist.span), start - d.first, end - d.first};
     for (int x0 = start; x0 < end; x0 += kWave * B) {
-      const int x = x0 + lane * B;  // this lane's first diagonal; what it sums beyond the end is left
-      float acc[B] = {};
-      for (int b = b0; b < b1; ++b) {
-        const T* rows = (const T*)g.data + b * g.batch_ld + h * g.head_ld;
-        // rows that meet the band at all
-        const int from = max(i0, -(x0 + kWave * B - 1)), to = (int)min((int64_t)i1, (int64_t)keys - x0);
-        for (int i = from + w * R; i < to; i += kSumWaves * R) {
-          const T* at = rows + i * g.query_ld + (i + x);  // a row on is a column on
-          VB v[R];
-          bool some[R], whole[R], inside = true;
+      if (!one_band) {
 #pragma unroll
-          for (int r = 0; r < R; ++r) {
-            const int j = i + r + x;
-            const T* q = at + r * (g.query_ld + 1);
-            some[r] = i + r < to && j + B > 0 && j < keys;
-            whole[r] = some[r] && q >= all.low && q + B <= all.high;
-            inside = inside && whole[r] && j >= 0 && j + B <= keys;
-            if (whole[r]) v[r] = *(const VB*)q;
-          }
-          if (__all(inside)) {
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-#pragma unroll
-              for (int k = 0; k < B; ++k) acc[k] += (float)v[r][k];
-            continue;
-          }
-#pragma unroll
-          for (int r = 0; r < R; ++r) {
-            if (!some[r]) continue;
-            const int j = i + r + x;
-#pragma unroll
-            for (int k = 0; k < B; ++k) {
-              if (j + k < 0 || j + k >= keys) continue;
-              acc[k] += whole[r] ? (float)v[r][k] : (float)at[r * (g.query_ld + 1) + k];
-            }
-          }
+        for (int k = 0; k < B; ++k) acc[k] = 0.f;
+        for (int b = b0; b < b1; ++b) {
+          const T* rows = (const T*)g.data + b * g.batch_ld + h * g.head_ld;
+          // rows that meet the band at all
+          const int from = max(i0, -(x0 + kWave * B - 1)), to = (int)min((int64_t)i1, (int64_t)keys - x0);
+          for (int i = from + w * R; i < to; i += kSumWaves * R) add_rows(rows, i, x0);
         }
       }
 #pragma unroll
