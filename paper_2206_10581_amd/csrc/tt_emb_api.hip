@@ -1006,7 +1006,7 @@ static bool good_ids(const int64_t* ids, int64_t B) { return B == 0 || (ids != n
 // ---- scores of logits, position bias ----
 
 constexpr int kTokenCols = 1 << 30;
-constexpr size_t kTokenSums = sizeof(f4) * kTokenParts, kTokenBytes = kTokenSums + sizeof(uint64_t) * kWave * kTokenParts;
+constexpr size_t kTokenLists = sizeof(f4) * kTokenParts, kTokenBytes = kTokenLists + sizeof(uint64_t) * kWave * kTokenParts;
 
 static bool good_floats(const void* p) { return ((uintptr_t)p & 3u) == 0; }
 static bool good_logits(const tt_emb_matrix* m, const int64_t* tokens, float scale) {
@@ -1401,8 +1401,8 @@ int tt_emb_token_scores(const tt_emb_matrix* logits, const int64_t* tokens, floa
   if (out->logprob != nullptr && tokens == nullptr) return TT_EMB_EINVAL;
   if (out->logprob == nullptr && out->entropy == nullptr && out->state == nullptr && !list) return TT_EMB_EINVAL;
   const TokenOut o{out->logprob, out->entropy, out->state, out->top_ids, out->top_logprob, list ? out->top : 0};
-  const TokenParts parts{(f4*)workspace, (unsigned long long*)((char*)workspace + kTokenSums)};
-  launch_token_scores(token_rows(*logits, tokens, scale), logits->type, o, parts, (hipStream_t)hip_stream);
+  launch_token_scores(token_rows(*logits, tokens, scale), logits->type, o,
+                      TokenParts{(f4*)workspace, (unsigned long long*)((char*)workspace + kTokenLists)}, (hipStream_t)hip_stream);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? TT_EMB_OK : hip_fail(e);
 }

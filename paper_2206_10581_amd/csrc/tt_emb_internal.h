@@ -587,11 +587,11 @@ struct TokenOut {
   float* top_logprob;
   int top;
 };
-struct TokenParts {
-  f4* sums;
-  unsigned long long* lists;
-};
 constexpr int kTokenParts = 1024;
+struct TokenParts {
+  f4* sums;                   // [kTokenParts]
+  unsigned long long* lists;  // [kTokenParts][kWave]
+};
 
 // Partial sums of a position bias's gradient (tt_emb_bias.hip): a part is a block's sums over the diagonals of `rows` rows
 // of one head and `group` sequences; a head has groups * chunks of them.

@@ -370,13 +370,18 @@ struct RowGradient {
 __device__ __forceinline__ RowGradient loss_gradient(const TokenRows& t, const Sums& s, float w, int64_t token) {
   return {s.most, __builtin_amdgcn_logf(s.sum), t.scale * w, 0.f, -t.scale * w, token, s.sum == 0.f};
 }
-template <bool ENT>
-__device__ __forceinline__ float gradient_of(const RowGradient& g, float x, int v, float c) {
-  const float y = fmaf(x - g.most, c, -g.logs2), p = pow2(y);
-  float d;
-  if constexpr (ENT) d = p * fmaf(g.b, fmaxf(y, kNothing), g.a);
-  else d = p * g.a;
-  return v == g.token ? d + g.token_part : d;
+template <bool ENT, int N>
+__device__ __forceinline__ void gradient_of(const RowGradient& g, float (&x)[N], int first, float c) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const float y = fmaf(x[i] - g.most, c, -g.logs2), p = pow2(y);
+    if constexpr (ENT) x[i] = p * fmaf(g.b, fmaxf(y, kNothing), g.a);
+    else x[i] = p * g.a;
+  }
+  if ((uint64_t)(g.token - first) < (uint64_t)N) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = first + i == g.token ? x[i] + g.token_part : x[i];
+  }
 }
 
 // ---- narrow rows: L lanes hold one, N pieces each
@@ -527,7 +532,11 @@ __global__ __launch_bounds__(kNarrowThreads) void k_token_loss_narrow(TokenRows 
       if (r.own[q] >= t.cols) continue;
       float v[P];
 #pragma unroll
-      for (int i = 0; i < P; ++i) v[i] = g.zero ? 0.f : gradient_of<false>(g, r.x[q * P + i], r.first[q] + i, t.c);
+      for (int i = 0; i < P; ++i) v[i] = r.x[q * P + i];
+      if (!g.zero) gradient_of<false>(g, v, r.first[q], t.c);
+      else
+#pragma unroll
+        for (int i = 0; i < P; ++i) v[i] = 0.f;
       TO* to = dx + row * ld_dx + r.first[q];
       if (t.cols >= P) store_piece<P, TO>(to, v);
       else
@@ -743,19 +752,24 @@ __device__ __forceinline__ void put_gradient(const RowGradient& g, const T* x, T
       for (int i = 0; i < P; ++i) v[i] = 0.f;
     } else {
       load_piece<P, T>(x + first, v);
-#pragma unroll
-      for (int i = 0; i < P; ++i) v[i] = gradient_of<ENT>(g, v[i], first + i, c);
+      gradient_of<ENT>(g, v, first, c);
     }
     store_piece<P, TO, true>(dx + first, v);
   }
   const int rest = from + pieces * P + thread;
-  if (rest < to) dx[rest] = (TO)(g.zero ? 0.f : gradient_of<ENT>(g, (float)x[rest], rest, c));
+  if (rest < to) {
+    float v[1] = {g.zero ? 0.f : (float)x[rest]};
+    if (!g.zero) gradient_of<ENT>(g, v, rest, c);
+    dx[rest] = (TO)v[0];
+  }
 }
 
 struct Upstream {
   const float *state, *entropy, *d_logprob, *d_entropy;
 };
 
+// The last rows first: what the scores read last may still be in the last-level cache (2744 rows of 32,000 bf16 behind their
+// scores 117 us, from the first on 120).
 constexpr int kGradThreads = 256;
 template <class T, class TO, bool ENT, int NT>
 __global__ __launch_bounds__(kGradThreads) void k_token_grad(TokenRows t, Upstream u, TO* dx, int64_t ld_dx,
@@ -763,8 +777,8 @@ __global__ __launch_bounds__(kGradThreads) void k_token_grad(TokenRows t, Upstre
   constexpr int kSide = kGradThreads / NT;  // rows beside each other in a block
   const int64_t work = t.rows * splits;
   for (int64_t b = (int64_t)blockIdx.x * kSide + threadIdx.x / NT; b < work; b += (int64_t)gridDim.x * kSide) {
-    const int64_t row = splits > 1 ? b / splits : b;
-    const int from = splits > 1 ? (int)(b - row * splits) * per : 0;
+    const int64_t back = splits > 1 ? b / splits : b, row = t.rows - 1 - back;
+    const int from = splits > 1 ? (int)(b - back * splits) * per : 0;
     const int64_t token = t.tokens ? t.tokens[row] : 0;
     RowGradient g{};
     g.zero = (uint64_t)token >= (uint64_t)t.cols;
@@ -823,19 +837,24 @@ static bool with_narrow(int cols, bool list, F&& f) {
   return true;
 }
 
-// How many blocks take a row of few rows, and how many columns each.
+// How many blocks take a row of few rows, and how many columns each.  Rows of up to two steps of a block are not shared: the second
+// launch costs more than it saves.  1 and 64 rows of 128,000 bf16 5.3 and 7.8 us shared by blocks of 512 threads, 10.4 and 12.2
+// by one of 1024 each; of 32,000 5.4 and 6.0, against 4.3 and 4.9; no difference from 129 rows of 128,000 on.
 static int splits_of(int64_t rows, int cols, int step, int* per) {
   int64_t n = std::min<int64_t>(kTokenParts / std::max<int64_t>(rows, 1), kWave);
   n = std::max<int64_t>(1, std::min<int64_t>(n, (cols + step / 2) / step));
+  if (n <= 2) n = 1;
   *per = (int)((cols + n - 1) / n + 7) / 8 * 8;
   return (cols + *per - 1) / *per;
 }
 
-template <class T, int NT, bool ENT>
-static void launch_wide(const TokenRows& t, const TokenOut& o, int splits, int per, const TokenParts& parts, hipStream_t st) {
-  const int blocks = grid_of(t.rows * splits);
-  if (o.top_ids) k_token_wide<T, NT, ENT, true><<<blocks, NT, 0, st>>>(t, o, splits, per, parts);
-  else k_token_wide<T, NT, ENT, false><<<blocks, NT, 0, st>>>(t, o, splits, per, parts);
+template <class T, int NT, bool TOP>
+static void launch_wide(const TokenRows& t, const TokenOut& o, const TokenParts& parts, hipStream_t st) {
+  int per;
+  const int splits = splits_of(t.rows, t.cols, NT * 64 / (int)sizeof(T), &per), blocks = grid_of(t.rows * splits);
+  if (o.entropy) k_token_wide<T, NT, true, TOP><<<blocks, NT, 0, st>>>(t, o, splits, per, parts);
+  else k_token_wide<T, NT, false, TOP><<<blocks, NT, 0, st>>>(t, o, splits, per, parts);
+  if (splits > 1) k_token_join<T, TOP><<<(int)t.rows, TOP ? 1024 : kWave, 0, st>>>(t, o, splits, parts);
 }
 
 void launch_token_scores(const TokenRows& t, int type, const TokenOut& o, const TokenParts& parts, hipStream_t st) {
@@ -846,14 +865,9 @@ void launch_token_scores(const TokenRows& t, int type, const TokenOut& o, const 
       k_token_narrow<T, L, N><<<grid_of((t.rows + kSide - 1) / kSide), kNarrowThreads, 0, st>>>(t, o);
     });
     if (narrow) return;
-    int per;
-    constexpr int NT = 256;
-    const int splits = splits_of(t.rows, t.cols, NT * 64 / (int)sizeof(T), &per);
-    if (o.entropy) launch_wide<T, NT, true>(t, o, splits, per, parts, st);
-    else launch_wide<T, NT, false>(t, o, splits, per, parts, st);
-    if (splits == 1) return;
-    if (o.top_ids) k_token_join<T, true><<<(int)t.rows, 1024, 0, st>>>(t, o, splits, parts);
-    else k_token_join<T, false><<<(int)t.rows, kWave, 0, st>>>(t, o, splits, parts);
+    // 4096 rows of 32,000 bf16 with entropy 33 us by blocks of 512 threads, 38 of 256; 48 of 128,000 with a list 25 and 21
+    if (o.top_ids) launch_wide<T, 256, true>(t, o, parts, st);
+    else launch_wide<T, 512, false>(t, o, parts, st);
   });
 }
 
@@ -868,7 +882,8 @@ static void launch_grad(const TokenRows& t, const Upstream& u, TO* dx, int64_t l
   auto sized = [&](auto ent) {
     if (t.cols <= 64) return go(ent, std::integral_constant<int, 16>{}, 1, t.cols);
     if (t.cols <= 1024) return go(ent, std::integral_constant<int, 64>{}, 1, t.cols);
-    const int per = 16384;
+    int per = 32768;  // columns of a block: as many as leave enough blocks
+    while (per > 8192 && t.rows * ((t.cols + per - 1) / per) < 2048) per /= 2;
     go(ent, std::integral_constant<int, kGradThreads>{}, (t.cols + per - 1) / per, per);
   };
   if (u.d_entropy) sized(std::true_type{});
