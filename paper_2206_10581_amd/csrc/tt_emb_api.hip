@@ -103,7 +103,7 @@ void launch_bias(const tt_emb_matrix& table, const tt_emb_distances&, float fill
                  const tt_emb_pairs& out, hipStream_t);
 SumPlan sum_plan(const tt_emb_pairs&, int span, bool offsets);
 void launch_bias_sums(const tt_emb_pairs&, const tt_emb_distances&, const tt_emb_matrix& out, bool add, const SumPlan&,
-                      double* total, PartReach* reach, float* parts, hipStream_t);
+                      const SumWork&, hipStream_t);
 hipError_t calibrate(void* buf, size_t bytes, hipStream_t, double* copy_bytes_per_s,
                      double* mfma_flops_per_s, double* gather_bytes_per_s,
                      double* far_gather_bytes_per_s);
@@ -1452,12 +1452,6 @@ int tt_emb_bias_forward(const tt_emb_matrix* table, const tt_emb_distances* dist
   return e == hipSuccess ? TT_EMB_OK : hip_fail(e);
 }
 
-// The totals of all distances and heads, what the parts reach, and the parts.
-struct SumWork {
-  double* total;
-  PartReach* reach;
-  float* parts;
-};
 static size_t carve_sums(const tt_emb_pairs& g, const SumPlan& p, int span, char* base, SumWork* ws) {
   size_t off = 0;
   auto take = [&](size_t bytes) {
@@ -1468,6 +1462,7 @@ static size_t carve_sums(const tt_emb_pairs& g, const SumPlan& p, int span, char
   if (p.parts == 0) return 0;
   SumWork w{};
   w.total = (double*)take((size_t)(2 * (int64_t)span + 1) * g.heads * sizeof(double));
+  w.reached = (int*)take((size_t)(2 * (int64_t)span + kWave) / kWave * sizeof(int));
   w.reach = (PartReach*)take((size_t)p.parts * sizeof(PartReach));
   w.parts = (float*)take((size_t)(p.parts * p.width) * sizeof(float));
   if (ws != nullptr) *ws = w;
@@ -1494,7 +1489,7 @@ int tt_emb_bias_backward(const tt_emb_pairs* grad, const tt_emb_distances* dista
     if (rc != TT_EMB_OK) return rc;
   }
   if (dtable->rows == 0) return TT_EMB_OK;
-  launch_bias_sums(*grad, *distances, *dtable, add != 0, plan, ws.total, ws.reach, ws.parts, (hipStream_t)hip_stream);
+  launch_bias_sums(*grad, *distances, *dtable, add != 0, plan, ws, (hipStream_t)hip_stream);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? TT_EMB_OK : hip_fail(e);
 }

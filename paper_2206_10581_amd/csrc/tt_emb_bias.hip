@@ -198,13 +198,13 @@ __global__ __launch_bounds__(kBiasThreads) void k_bias_tiles(tt_emb_matrix table
 
 // ---- sums of buckets
 
-// The diagonals d = j - i of a sequence that are told apart: [first, last], where first stands for all before it, too, and
+// The diagonals d = j - i of rows [i0, i1) that are told apart: [first, last], where first stands for all before it, too, and
 // last for all behind.
 struct Span {
   int first, last;
 };
-__device__ __forceinline__ Span span_of(const tt_emb_pairs& g, int64_t offset, int span) {
-  const int64_t low = 1 - g.queries, high = g.keys - 1;
+__device__ __forceinline__ Span span_of(int i0, int i1, int keys, int64_t offset, int span) {
+  const int64_t low = 1 - i1, high = keys - 1 - i0;
   return {(int)min(max(-(int64_t)span - offset, low), high), (int)max(min((int64_t)span - offset, high), low)};
 }
 
@@ -215,6 +215,81 @@ __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll
   for (int d = kWave / 2; d > 0; d /= 2) v += __shfl_xor(v, d);
   return v;
+}
+
+// What a part sums: rows [i0, i1) of sequences [b0, b1) in head h.
+struct PartPlace {
+  int h, b0, b1, i0, i1;
+  __device__ __forceinline__ PartPlace(const SumPlan& p, const tt_emb_pairs& g, int64_t part) {
+    const int64_t plane = quotient(part, p.chunks);
+    const int chunk = (int)(part - plane * p.chunks);
+    h = (int)quotient(plane, p.groups);
+    b0 = (int)(plane - (int64_t)h * p.groups) * p.group;
+    b1 = min(b0 + p.group, g.batch);
+    i0 = chunk * p.rows;
+    i1 = (int)min((int64_t)i0 + p.rows, g.queries);
+  }
+};
+
+// The sums of all before and behind, of a block's wavefronts, to the ends of its part.
+__device__ __forceinline__ void put_ends(float before, float behind, const Span& d, float* __restrict__ out) {
+  __shared__ float ends[kSumWaves][2];
+  before = wave_sum(before);
+  behind = wave_sum(behind);
+  if (threadIdx.x % kWave == 0) {
+    ends[threadIdx.x / kWave][0] = before;
+    ends[threadIdx.x / kWave][1] = behind;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    float a = 0.f, z = 0.f;
+    for (int k = 0; k < kSumWaves; ++k) {
+      a += ends[k][0];
+      z += ends[k][1];
+    }
+    if (d.first == d.last) {
+      out[0] = a + z;
+    } else {
+      out[0] = a;
+      out[d.last - d.first] = z;
+    }
+  }
+  __syncthreads();
+}
+
+// Short rows: a thread has a diagonal, which holds no more values than a row.
+constexpr int kShortKeys = 64;
+template <class T>
+__global__ __launch_bounds__(kSumThreads) void k_bias_sums_short(tt_emb_pairs g, tt_emb_distances dist, SumPlan p,
+                                                                 float* __restrict__ parts, PartReach* __restrict__ reach) {
+  constexpr int kAhead = 4;
+  for (int64_t part = blockIdx.x; part < p.parts; part += gridDim.x) {
+    const PartPlace t(p, g, part);
+    const int keys = (int)g.keys;
+    const int64_t offset = offset_of(dist, t.b0);
+    const Span d = span_of(t.i0, t.i1, keys, offset, dist.span);
+    float* out = parts + part * p.width;
+    if (threadIdx.x == 0) reach[part] = PartReach{cut(d.first + offset, dist.span), cut(d.last + offset, dist.span)};
+    float before = 0.f, behind = 0.f;
+    for (int x = 1 - t.i1 + (int)threadIdx.x; x < keys - t.i0; x += kSumThreads) {
+      const int from = max(t.i0, -x), to = min(t.i1, keys - x);
+      float sum = 0.f;
+      for (int b = t.b0; b < t.b1; ++b) {
+        const T* at = (const T*)g.data + b * g.batch_ld + t.h * g.head_ld + x;
+        for (int i = from; i < to; i += kAhead) {
+          float v[kAhead];
+#pragma unroll
+          for (int n = 0; n < kAhead; ++n) v[n] = (float)at[min(i + n, to - 1) * (g.query_ld + 1)];
+#pragma unroll
+          for (int n = 0; n < kAhead; ++n) sum += i + n < to ? v[n] : 0.f;
+        }
+      }
+      if (x <= d.first) before += sum;
+      else if (x >= d.last) behind += sum;
+      else out[x - d.first] = sum;
+    }
+    put_ends(before, behind, d, out);
+  }
 }
 
 // Where a gradient's memory starts and ends: pieces may reach over a row's ends, but not over these.
@@ -270,23 +345,20 @@ __global__ __launch_bounds__(kSumThreads) void k_bias_sums(tt_emb_pairs g, tt_em
   const int lane = threadIdx.x % kWave, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
   const Extent<T> all(g);
   for (int64_t part = blockIdx.x; part < p.parts; part += gridDim.x) {
-    const int64_t plane = quotient(part, p.chunks);
-    const int chunk = (int)(part - plane * p.chunks);
-    const int h = (int)quotient(plane, p.groups), b0 = (int)(plane - (int64_t)h * p.groups) * p.group;
-    const int b1 = min(b0 + p.group, g.batch), i0 = chunk * p.rows, i1 = (int)min((int64_t)i0 + p.rows, g.queries);
+    const PartPlace t(p, g, part);
+    const int h = t.h, b0 = t.b0, b1 = t.b1, i0 = t.i0, i1 = t.i1;
     const int keys = (int)g.keys;
     const int64_t offset = offset_of(dist, b0);
-    const Span d = span_of(g, offset, dist.span);
+    const Span d = span_of(i0, i1, keys, offset, dist.span);
     float* out = parts + part * p.width;
     auto wanted = [&](int diagonal) {
       return (uint32_t)dist.bucket_of[cut(diagonal + offset, dist.span) + dist.span] < (uint32_t)buckets;
     };
     const bool low = wanted(d.first), high = wanted(d.last);
     float before = 0.f, behind = 0.f;
-    // what lies between, as far as these rows reach: R rows of the band of 64 B diagonals from x0 on
-    const int start = max(d.first + 1, 1 - i1), end = min(d.last, keys - i0);
-    if (threadIdx.x == 0)
-      reach[part] = PartReach{cut(d.first + offset, dist.span), cut(d.last + offset, dist.span), start - d.first, end - d.first};
+    if (threadIdx.x == 0) reach[part] = PartReach{cut(d.first + offset, dist.span), cut(d.last + offset, dist.span)};
+    // what lies between: R rows of the band of 64 B diagonals from x0 on
+    const int start = d.first + 1, end = d.last;
     float acc[B] = {};
     auto add_rows = [&](const T* rows, int i, int x0) {
       const int x = x0 + lane * B, to = (int)min((int64_t)i1, (int64_t)keys - x0);  // this lane's first diagonal
@@ -302,12 +374,15 @@ __global__ __launch_bounds__(kSumThreads) void k_bias_sums(tt_emb_pairs g, tt_em
           for (int k = 0; k < B; ++k) acc[k] += (float)v[r][k];
         return;
       }
+      const T* first = rows + i * g.query_ld + (i + x0);
+      // whether pieces that reach over the rows' ends stay within the memory, for all lanes
+      const bool safe = first >= all.low && first + (R - 1) * (g.query_ld + 1) + kWave * B <= all.high;
       bool cut_off = false;
 #pragma unroll
       for (int r = 0; r < R; ++r) {
         const int j = i + r + x;
         const T* q = at + r * (g.query_ld + 1);
-        const bool some = i + r < to && j + B > 0 && j < keys, whole = some && q >= all.low && q + B <= all.high;
+        const bool some = i + r < to && j + B > 0 && j < keys, whole = some && (safe || (q >= all.low && q + B <= all.high));
         v[r] = VB{};
         if (whole) v[r] = *(const VB*)q;
         cut_off = cut_off || (some && !whole);
@@ -385,27 +460,7 @@ __global__ __launch_bounds__(kSumThreads) void k_bias_sums(tt_emb_pairs g, tt_em
         if (one_band) add_rows(rows, i, start);
       }
     }
-    before = wave_sum(before);
-    behind = wave_sum(behind);
-    if (lane == 0) {
-      sums[w][0] = before;
-      sums[w][1] = behind;
-    }
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      float a = 0.f, z = 0.f;
-      for (int k = 0; k < kSumWaves; ++k) {
-        a += sums[k][0];
-        z += sums[k][1];
-      }
-      if (d.first == d.last) {
-        out[0] = a + z;
-      } else {
-        out[0] = a;
-        out[d.last - d.first] = z;
-      }
-    }
-    __syncthreads();
+    put_ends(before, behind, d, out);
     for (int x0 = start; x0 < end; x0 += kWave * B) {
       if (!one_band) {
 #pragma unroll
@@ -431,81 +486,125 @@ __global__ __launch_bounds__(kSumThreads) void k_bias_sums(tt_emb_pairs g, tt_em
   }
 }
 
-// total[distance][head]: all parts of a head and distance, in fp64.  A block has 64 distances, a wavefront every 16th part.
-constexpr int kJoinThreads = 1024, kJoinWaves = kJoinThreads / kWave, kJoinAhead = 8;
-__global__ __launch_bounds__(kJoinThreads) void k_bias_join(int heads, int span, SumPlan p, const float* __restrict__ parts,
-                                                            const PartReach* __restrict__ reach, double* __restrict__ total) {
-  __shared__ double sums[kJoinWaves][kWave];
+// total[head][distance - low]: all parts of a head and distance, in fp64, of `count` distances from `low` on.  A block has 64 of
+// them, a wavefront some of the parts; those that a part tells apart, or stands for, are one behind the other in it.
+// reached: which blocks' distances any part has, for any head.
+constexpr int kJoinAhead = 8;
+template <int W>
+__global__ __launch_bounds__(W * kWave) void k_bias_join(int heads, int low, int count, SumPlan p,
+                                                         const float* __restrict__ parts, const PartReach* __restrict__ reach,
+                                                         double* __restrict__ total, int* __restrict__ reached) {
+  __shared__ double sums[W][kWave];
+  __shared__ int any[W];
   const int lane = threadIdx.x % kWave, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
-  const int per_head = p.groups * p.chunks, distances = 2 * span + 1, tiles = (distances + kWave - 1) / kWave;
+  const int per_head = p.groups * p.chunks, tiles = (count + kWave - 1) / kWave;
   for (int64_t tile = blockIdx.x; tile < (int64_t)tiles * heads; tile += gridDim.x) {
-    const int h = (int)quotient(tile, tiles), r = (int)(tile - (int64_t)h * tiles) * kWave + lane, distance = r - span;
+    const int h = (int)quotient(tile, tiles), t = (int)(tile - (int64_t)h * tiles), r = t * kWave + lane, distance = low + r;
     double sum = 0.0;
-    for (int k0 = w; k0 < per_head; k0 += kJoinWaves * kJoinAhead) {
+    bool has = false;
+    for (int k0 = w; k0 < per_head; k0 += W * kJoinAhead) {
       PartReach a[kJoinAhead];
       float v[kJoinAhead];
 #pragma unroll
-      for (int n = 0; n < kJoinAhead; ++n) a[n] = reach[(int64_t)h * per_head + min(k0 + n * kJoinWaves, per_head - 1)];
+      for (int n = 0; n < kJoinAhead; ++n) a[n] = reach[(int64_t)h * per_head + min(k0 + n * W, per_head - 1)];
 #pragma unroll
       for (int n = 0; n < kJoinAhead; ++n) {
-        const int k = k0 + n * kJoinWaves, at = distance - a[n].first, last = a[n].last - a[n].first;
+        const int k = k0 + n * W;
         v[n] = 0.f;
-        if (k < per_head && r < distances && (at == 0 || at == last || (at > 0 && at < last && at >= a[n].start && at < a[n].end)))
-          v[n] = parts[((int64_t)h * per_head + k) * p.width + at];
+        if (k < per_head && r < count && distance >= a[n].first && distance <= a[n].last) {
+          v[n] = parts[((int64_t)h * per_head + k) * p.width + (distance - a[n].first)];
+          has = true;
+        }
       }
 #pragma unroll
       for (int n = 0; n < kJoinAhead; ++n) sum += (double)v[n];
     }
     sums[w][lane] = sum;
+    const int some = __any(has);
+    if (lane == 0) any[w] = some;
     __syncthreads();
-    if (w == 0 && r < distances) {
+    if (w == 0) {
       sum = 0.0;
+      int all = 0;
 #pragma unroll
-      for (int k = 0; k < kJoinWaves; ++k) sum += sums[k][lane];
-      total[(int64_t)r * heads + h] = sum;
+      for (int k = 0; k < W; ++k) {
+        sum += sums[k][lane];
+        all |= any[k];
+      }
+      if (all && r < count) total[(int64_t)h * count + r] = sum;
+      if (h == 0 && lane == 0) reached[t] = all;
     }
     __syncthreads();
   }
 }
 
-// A block adds up the distances of one bucket, threads side by side over the heads.
-template <class TO>
-__global__ __launch_bounds__(kSumThreads) void k_bias_buckets(int heads, tt_emb_distances dist, const double* __restrict__ total,
-                                                              TO* __restrict__ out, int64_t ld, int buckets, bool add,
-                                                              int lanes) {
-  __shared__ int found[kSumThreads], counts[kSumWaves];
-  __shared__ double sums[kSumThreads];
-  const int lane = threadIdx.x % kWave, w = threadIdx.x / kWave, distances = total ? 2 * dist.span + 1 : 0;
-  const int side = threadIdx.x & ((1 << lanes) - 1), up = threadIdx.x >> lanes, step = kSumThreads >> lanes;
+// A block adds up the distances of one bucket in all heads: W * 64 * U at a time, first which they are, in order, then their
+// totals, of few by a thread for each head, of more by a wavefront.
+constexpr int kFewDistances = 16;
+template <class TO, int W, int U>
+__global__ __launch_bounds__(W * kWave) void k_bias_buckets(int heads, const int32_t* __restrict__ bucket_of, int count,
+                                                            const double* __restrict__ total, const int* __restrict__ reached,
+                                                            TO* __restrict__ out, int64_t ld, int buckets, bool add) {
+  constexpr int kThreads = W * kWave, kAhead = 4;
+  __shared__ int found[U * kThreads], counts[kWave];
+  __shared__ double sums[kThreads];  // of heads h0, h0 + 1, ...
+  static_assert(U * W <= kWave, "a count for each lane");
+  const int lane = threadIdx.x % kWave, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
   for (int u = blockIdx.x; u < buckets; u += gridDim.x)
-    for (int h0 = 0; h0 < heads; h0 += 1 << lanes) {
-      const int h = h0 + side;
-      double sum = 0.0;
-      for (int r0 = 0; r0 < distances; r0 += kSumThreads) {
-        const int r = r0 + (int)threadIdx.x;
-        const uint64_t mask = __ballot(dist.bucket_of[min(r, distances - 1)] == u && r < distances);
-        if (lane == 0) counts[w] = __popcll(mask);
-        __syncthreads();
-        int before = 0, n = 0;
+    for (int h0 = 0; h0 < heads; h0 += kThreads) {
+      sums[threadIdx.x] = 0.0;
+      for (int r0 = 0; r0 < count; r0 += U * kThreads) {
+        uint64_t mask[U];
 #pragma unroll
-        for (int k = 0; k < kSumWaves; ++k) {
-          before += k < w ? counts[k] : 0;
-          n += counts[k];
+        for (int n = 0; n < U; ++n) {
+          const int r = r0 + n * kThreads + (int)threadIdx.x, at = min(r, count - 1);
+          mask[n] = __ballot((int)(bucket_of[at] == u) & (int)(reached[at / kWave] != 0) & (int)(r < count));
+          if (lane == 0) counts[n * W + w] = __popcll(mask[n]);
         }
-        if (mask >> lane & 1) found[before + __popcll(mask & ((uint64_t(1) << lane) - 1))] = r;
         __syncthreads();
-        if (h < heads)
-          for (int m = up; m < n; m += step) sum += total[(int64_t)found[m] * heads + h];
+        const int mine = lane < U * W ? counts[lane] : 0;
+        int all = mine;  // of this place and all before it
+#pragma unroll
+        for (int k = 1; k < kWave; k *= 2) {
+          const int before = __shfl_up(all, k);
+          all += lane >= k ? before : 0;
+        }
+#pragma unroll
+        for (int n = 0; n < U; ++n) {
+          const int from = __builtin_amdgcn_readlane(all - mine, n * W + w);
+          if (mask[n] >> lane & 1)
+            found[from + __popcll(mask[n] & ((uint64_t(1) << lane) - 1))] = r0 + n * kThreads + (int)threadIdx.x;
+        }
+        const int n = __builtin_amdgcn_readlane(all, kWave - 1);
+        __syncthreads();
+        if (n <= kFewDistances) {
+          const int h = h0 + (int)threadIdx.x;
+          double sum = 0.0;
+          if (h < heads)
+            for (int m = 0; m < n; ++m) sum += total[(int64_t)h * count + found[m]];
+          sums[threadIdx.x] += sum;
+        } else {
+          for (int h = h0 + w; h < min(heads, h0 + kThreads); h += W) {
+            double sum = 0.0;
+            for (int m = lane; m < n; m += kAhead * kWave) {
+              double v[kAhead];
+#pragma unroll
+              for (int k = 0; k < kAhead; ++k) v[k] = total[(int64_t)h * count + found[min(m + k * kWave, n - 1)]];
+#pragma unroll
+              for (int k = 0; k < kAhead; ++k) sum += m + k * kWave < n ? v[k] : 0.0;
+            }
+#pragma unroll
+            for (int k = kWave / 2; k > 0; k /= 2) sum += __shfl_xor(sum, k);
+            if (lane == 0) sums[h - h0] += sum;
+          }
+        }
         __syncthreads();
       }
-      sums[threadIdx.x] = sum;
-      __syncthreads();
-      if (up == 0 && h < heads) {
-        for (int k = 1; k < step; ++k) sum += sums[(k << lanes) + side];
+      const int h = h0 + (int)threadIdx.x;
+      if (h < heads) {
         TO* to = out + u * ld + h;
-        *to = (TO)(float)(add ? (double)(float)*to + sum : sum);
+        *to = (TO)(float)(add ? (double)(float)*to + sums[threadIdx.x] : sums[threadIdx.x]);
       }
-      __syncthreads();
     }
 }
 
@@ -552,39 +651,61 @@ SumPlan sum_plan(const tt_emb_pairs& g, int span, bool offsets) {
   SumPlan p{};
   const int64_t batch = g.batch, heads = g.heads;
   if (batch == 0 || heads == 0 || g.queries == 0 || g.keys == 0) return p;
-  p.width = std::min<int64_t>(g.queries + g.keys - 1, 2 * (int64_t)span + 1);
-  // parts of a head: enough blocks, each with eight times the values that it leaves
-  const int64_t places = batch * g.queries * g.keys;
-  const int64_t want = std::max<int64_t>(1, std::min<int64_t>(kSumParts / heads, places / (8 * p.width)));
+  // parts of a head: enough blocks, of 16 rows at least
+  const int64_t want = std::max<int64_t>(1, std::min<int64_t>(kSumParts / heads, batch * ((g.queries + 15) / 16)));
   p.group = offsets ? 1 : (int)((batch + want - 1) / want);
   p.groups = (int)((batch + p.group - 1) / p.group);
   const int64_t chunks = std::max<int64_t>(1, std::min<int64_t>(want / p.groups, (g.queries + 15) / 16));
   p.rows = (int)((g.queries + chunks - 1) / chunks);
   p.chunks = (int)((g.queries + p.rows - 1) / p.rows);
+  p.width = std::min<int64_t>(p.rows + g.keys - 1, 2 * (int64_t)span + 1);
   p.parts = heads * p.groups * p.chunks;
   return p;
 }
 
+// Distances [low, low + count) that may occur: with one offset for all sequences no others have to be joined.
+static void distances_of(const tt_emb_pairs& g, const tt_emb_distances& dist, int* low, int* count) {
+  int64_t from = -(int64_t)dist.span, to = dist.span;
+  if (dist.offsets == nullptr) {
+    const int64_t far = int64_t(1) << 40, o = std::min(std::max(dist.offset, -far), far);
+    from = std::min(std::max(o + 1 - g.queries, from), to);
+    to = std::max(std::min(o + g.keys - 1, to), from);
+  }
+  *low = (int)from;
+  *count = (int)(to - from) + 1;
+}
+
 void launch_bias_sums(const tt_emb_pairs& g, const tt_emb_distances& dist, const tt_emb_matrix& out, bool add,
-                      const SumPlan& p, double* total, PartReach* reach, float* parts, hipStream_t st) {
+                      const SumPlan& p, const SumWork& ws, hipStream_t st) {
+  int low = 0, count = 0;
   if (p.parts > 0) {
     with_type(g.type, [&](auto t) {
       typedef decltype(t) T;
       const int blocks = (int)std::min(p.parts, kMostBlocks);
-      if (p.width - 2 <= kWave * 4)
-        k_bias_sums<T, 4><<<blocks, kSumThreads, 0, st>>>(g, dist, (int)out.rows, p, parts, reach);
+      if (g.keys <= kShortKeys)
+        k_bias_sums_short<T><<<blocks, kSumThreads, 0, st>>>(g, dist, p, ws.parts, ws.reach);
+      else if (p.width - 2 <= kWave * 4)
+        k_bias_sums<T, 4><<<blocks, kSumThreads, 0, st>>>(g, dist, (int)out.rows, p, ws.parts, ws.reach);
       else
-        k_bias_sums<T, 8><<<blocks, kSumThreads, 0, st>>>(g, dist, (int)out.rows, p, parts, reach);
+        k_bias_sums<T, 8><<<blocks, kSumThreads, 0, st>>>(g, dist, (int)out.rows, p, ws.parts, ws.reach);
     });
-    const int64_t tiles = (2 * (int64_t)dist.span + kWave) / kWave * g.heads;
-    k_bias_join<<<(int)std::min(tiles, kMostBlocks), kJoinThreads, 0, st>>>(g.heads, dist.span, p, parts, reach, total);
+    distances_of(g, dist, &low, &count);
+    const int blocks = (int)std::min<int64_t>((int64_t)(count + kWave - 1) / kWave * g.heads, kMostBlocks);
+    if (blocks >= 1024)
+      k_bias_join<4><<<blocks, 4 * kWave, 0, st>>>(g.heads, low, count, p, ws.parts, ws.reach, ws.total, ws.reached);
+    else
+      k_bias_join<16><<<blocks, 16 * kWave, 0, st>>>(g.heads, low, count, p, ws.parts, ws.reach, ws.total, ws.reached);
   }
-  int lanes = 0;
-  while ((1 << lanes) < kWave && (1 << lanes) < g.heads) ++lanes;
   with_type(out.type, [&](auto t) {
     typedef decltype(t) TO;
-    k_bias_buckets<TO><<<(int)std::min(out.rows, kMostBlocks), kSumThreads, 0, st>>>(
-        g.heads, dist, p.parts > 0 ? total : nullptr, (TO*)out.data, out.ld, (int)out.rows, add, lanes);
+    auto go = [&](auto waves, auto ahead) {
+      constexpr int W = decltype(waves)::value, U = decltype(ahead)::value;
+      k_bias_buckets<TO, W, U><<<(int)std::min(out.rows, kMostBlocks), W * kWave, 0, st>>>(
+          g.heads, dist.bucket_of + dist.span + low, count, ws.total, ws.reached, (TO*)out.data, out.ld, (int)out.rows, add);
+    };
+    if (count <= 1024) go(std::integral_constant<int, 4>{}, std::integral_constant<int, 4>{});
+    else if (out.rows >= 512) go(std::integral_constant<int, 4>{}, std::integral_constant<int, 16>{});
+    else go(std::integral_constant<int, 16>{}, std::integral_constant<int, 4>{});
   });
 }
 

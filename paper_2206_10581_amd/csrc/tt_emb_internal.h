@@ -600,9 +600,15 @@ struct SumPlan {
   int group, groups, rows, chunks;
 };
 constexpr int kSumParts = 2048;  // about as many at most
-// The distances that a part's first and last value stand for; of those between, values [start, end) are there, the others zero.
+// The distances that a part's first and last value stand for.
 struct PartReach {
-  int first, last, start, end;
+  int first, last;
+};
+struct SumWork {
+  double* total;     // [heads][distances], of those that occur
+  int* reached;      // [distances / kWave]: whether any of them occurs
+  PartReach* reach;  // [parts]
+  float* parts;      // [parts][width]
 };
 
 inline int type_size(int type) { return type == TT_EMB_FP32 ? 4 : 2; }

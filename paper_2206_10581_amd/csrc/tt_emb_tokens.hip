@@ -426,16 +426,20 @@ struct NarrowRow {
   }
   template <bool ENT>
   __device__ __forceinline__ Sums sums(int cols, float c) const {
-    float v[N * P], most = kLowest;
+    float v[N][P], most = kLowest;
 #pragma unroll
     for (int q = 0; q < N; ++q)
+      if (q * L * P < cols) {  // the same for all lanes
 #pragma unroll
-      for (int i = 0; i < P; ++i) {
-        v[q * P + i] = mine(q, i, cols) ? x[q * P + i] : -INFINITY;
-        most = fmaxf(most, v[q * P + i]);
+        for (int i = 0; i < P; ++i) {
+          v[q][i] = mine(q, i, cols) ? x[q * P + i] : -INFINITY;
+          most = fmaxf(most, v[q][i]);
+        }
       }
     Sums s{most, 0.f, 0.f};
-    add_values<ENT>(s, v, most, c);
+#pragma unroll
+    for (int q = 0; q < N; ++q)
+      if (q * L * P < cols) add_values<ENT>(s, v[q], most, c);
     join_lanes<ENT, L>(s, c);
     return s;
   }

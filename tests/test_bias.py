@@ -33,6 +33,8 @@ def _map(how):
         return tt.PositionBias.log_buckets(32, 5000), 32
     if how == "each":
         return torch.arange(401, dtype=torch.int32), 401
+    if how == "wide":                         # a bucket for each of 3001 distances
+        return torch.arange(3001, dtype=torch.int32), 3001
     if how == "one":
         return torch.zeros(1, dtype=torch.int32), 1
     if how == "mixed":                        # no order, holes, buckets that nothing names, numbers outside the table
@@ -58,6 +60,11 @@ def _buckets(of, offset, batch, queries, keys):
 MAPS = ["both", "causal", "far", "each", "one", "mixed", "none"]
 # batch, heads, queries, keys
 SIZES = [(1, 1, 1, 1), (3, 2, 1, 300), (2, 3, 40, 1), (2, 3, 17, 33), (1, 2, 129, 515), (2, 1, 300, 1100), (5, 2, 64, 64), (1, 3, 7, 2051)]
+
+
+# many heads, so that a part holds several sequences; short rows; many buckets
+MORE = [("both", (20, 300, 7, 40)), ("each", (9, 70, 33, 100)), ("both", (2, 3, 2000, 5)), ("causal", (3, 2, 2500, 64)),
+        ("wide", (2, 5, 300, 1100)), ("wide", (2, 3, 700, 20)), ("far", (3, 300, 9, 300))]
 
 
 def _offsets(kind, batch, queries, keys):
@@ -126,8 +133,7 @@ def _roundings(batch, queries, keys):
     return 24 + batch * (queries / 4 + 4) * (keys / 256 + 2)
 
 
-@pytest.mark.parametrize("size", SIZES)
-@pytest.mark.parametrize("how", MAPS)
+@pytest.mark.parametrize("how,size", [(how, size) for how in MAPS for size in SIZES] + MORE)
 def test_gradient(how, size):
     import torch
     import paper_2206_10581_amd as tt
