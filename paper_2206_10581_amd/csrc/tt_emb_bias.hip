@@ -257,8 +257,11 @@ __device__ __forceinline__ void put_ends(float before, float behind, const Span&
   __syncthreads();
 }
 
-// Short rows: a thread has a diagonal, which holds no more values than a row.
-constexpr int kShortKeys = 64;
+// Short rows: a thread has a diagonal, which holds no more values than a row.  Bound by the requests to the caches, each of
+// which brings 64 rows' lines: up to 64 keys, and to 512 where a part has few rows.  Against bands, us: 34 x 9 x 3022 x 40 bf16 66 / 165,
+// x 66 184 / 182 (503 rows a part), 16 x 9 x 3022 x 128 134 / 104 (216), x 1022 x 100 fp32 33 / 41 (73), 8 x 16 x 1000 x 256 bf16
+// 38 / 45 (63), x 200 x 500 19 / 23 (25).
+constexpr int kShortKeys = 64, kShortRow = 512, kShortRows = 128;
 template <class T>
 __global__ __launch_bounds__(kSumThreads) void k_bias_sums_short(tt_emb_pairs g, tt_emb_distances dist, SumPlan p,
                                                                  float* __restrict__ parts, PartReach* __restrict__ reach) {
@@ -682,7 +685,7 @@ void launch_bias_sums(const tt_emb_pairs& g, const tt_emb_distances& dist, const
     with_type(g.type, [&](auto t) {
       typedef decltype(t) T;
       const int blocks = (int)std::min(p.parts, kMostBlocks);
-      if (g.keys <= kShortKeys)
+      if (g.keys <= kShortKeys || (g.keys <= kShortRow && p.rows <= kShortRows))
         k_bias_sums_short<T><<<blocks, kSumThreads, 0, st>>>(g, dist, p, ws.parts, ws.reach);
       else if (p.width - 2 <= kWave * 4)
         k_bias_sums<T, 4><<<blocks, kSumThreads, 0, st>>>(g, dist, (int)out.rows, p, ws.parts, ws.reach);
