@@ -356,7 +356,7 @@ int tt_emb_token_workspace_bytes(size_t* bytes);
  * the likeliest tokens.  logits: rows below 2^30 and 1 .. 2^30 columns (a vocabulary, classes).  tokens: device
  * int64[rows]; a row whose token is outside [0, cols) is left out: it is not read, and has log probability
  * and entropy 0 and no likely tokens (id -1, log probability -infinity, as in the places behind the last column).  tokens null:
- * all rows count.  scale > 0, finite (1 / temperature).  Sums are held in fp32 relative to the row's largest logit, in an order
+ * all rows count.  0 < scale <= 1e38 (1 / temperature).  Sums are held in fp32 relative to the row's largest logit, in an order
  * that the sizes alone fix; any logit may be -infinity (probability 0).  A row of -infinity alone has log probability -infinity,
  * entropy 0 and no gradient; one with NaN or +infinity has NaN (and among the likeliest NaN comes before +infinity).
  * workspace: device, 256-byte aligned; calls that share one must be ordered by a stream.  May be captured

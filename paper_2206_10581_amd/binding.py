@@ -788,8 +788,8 @@ class TokenScores(_OnDevice):
             device = torch.device("cuda", torch.cuda.current_device())
         super().__init__(device)
         self.scale = float(scale)
-        if not 0.0 < self.scale < math.inf:
-            raise ValueError(f"scale {scale}: positive and finite needed")
+        if not 0.0 < self.scale <= 1e38:
+            raise ValueError(f"scale {scale}: a positive number up to 1e38 needed")
         rc, nbytes = tt_emb_token_workspace_bytes()
         if rc:
             raise TTEmbError(rc, "tt_emb_token_workspace_bytes")

@@ -1010,7 +1010,7 @@ constexpr size_t kTokenLists = sizeof(f4) * kTokenParts, kTokenBytes = kTokenLis
 
 static bool good_floats(const void* p) { return ((uintptr_t)p & 3u) == 0; }
 static bool good_logits(const tt_emb_matrix* m, const int64_t* tokens, float scale) {
-  return good_matrix(m, kDenseBatch, kTokenCols) && ((uintptr_t)tokens & 7u) == 0 && scale > 0.f && std::isfinite(scale);
+  return good_matrix(m, kDenseBatch, kTokenCols) && ((uintptr_t)tokens & 7u) == 0 && scale > 0.f && scale <= 1e38f;  // scale / log 2 has to be a number
 }
 static TokenRows token_rows(const tt_emb_matrix& m, const int64_t* tokens, float scale) {
   return {m.data, m.ld, m.rows, m.cols, tokens, scale, (float)((double)scale * 1.4426950408889634)};

@@ -129,69 +129,79 @@ __global__ __launch_bounds__(kBiasThreads) void k_bias_tiles(tt_emb_matrix table
     const int rows = (int)min((int64_t)tl.rows, out.queries - i0), cols = (int)min((int64_t)tl.cols, out.keys - j0);
     const int64_t first = offset_of(dist, b) + j0 - i0 - (rows - 1);  // distance of the first diagonal
     const Values values{table, dist.bucket_of, dist.span, h, fill};
+    const TI* from = (const TI*)in.data + (ADD ? b * in.batch_ld + h * in.head_ld + i0 * in.query_ld + j0 : 0);
+    TO* to = (TO*)out.data + b * out.batch_ld + h * out.head_ld + i0 * out.query_ld + j0;
+    const int c = side * P;  // a tile is no wider than the block's threads
+    const bool whole = c + P <= cols;
+    typedef typename Piece<TI, P>::V V;
+    auto load_rows = [&](int r0, V(&v)[R]) {
+      if constexpr (ADD)
+        if (whole && r0 < rows) {
+#pragma unroll
+          for (int k = 0; k < R; ++k) v[k] = *(const V*)(from + min(r0 + k * step, rows - 1) * in.query_ld + c);
+        }
+    };
+    V v[R], next[R];
+    load_rows(up, v);
     const bool one = first >= dist.span || first + rows + cols - 2 <= -dist.span;
     float all = 0.f;
     if (one) {
       all = values.of(values.bucket(first));
     } else {
       for (int x0 = threadIdx.x; x0 < rows + cols - 1; x0 += kAhead * kBiasThreads) {
-        float v[kAhead];
-        values.get(first + x0, kBiasThreads, v);
+        float w[kAhead];
+        values.get(first + x0, kBiasThreads, w);
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
           const int x = x0 + k * kBiasThreads;
           if (x >= rows + cols - 1) continue;
 #pragma unroll
           for (int s = 0; s < 4; ++s)
-            if (x >= s) lines[word(s, (x - s) / 4) + (x - s) % 4] = v[k];
+            if (x >= s) lines[word(s, (x - s) / 4) + (x - s) % 4] = w[k];
         }
       }
       __syncthreads();
     }
-    const TI* from = (const TI*)in.data + (ADD ? b * in.batch_ld + h * in.head_ld + i0 * in.query_ld + j0 : 0);
-    TO* to = (TO*)out.data + b * out.batch_ld + h * out.head_ld + i0 * out.query_ld + j0;
-    for (int r0 = up; r0 < rows; r0 += step * R)
-      for (int c = side * P; c < cols; c += P << tl.lanes) {
-        if (c + P > cols) {  // cut off
-          for (int r = r0; r < rows && r < r0 + step * R; r += step)
-            for (int i = c; i < cols; ++i) {
-              const int a = i - r + rows - 1;
-              float y = one ? all : lines[word(0, a / 4) + a % 4];
-              if constexpr (ADD) y = added((float)from[r * in.query_ld + i], y);
-              to[r * out.query_ld + i] = (TO)y;
-            }
-          continue;
+    for (int r0 = up; r0 < rows && c < cols; r0 += step * R) {
+      if (!whole) {  // cut off
+        for (int r = r0; r < rows && r < r0 + step * R; r += step)
+          for (int i = c; i < cols; ++i) {
+            const int a = i - r + rows - 1;
+            float y = one ? all : lines[word(0, a / 4) + a % 4];
+            if constexpr (ADD) y = added((float)from[r * in.query_ld + i], y);
+            to[r * out.query_ld + i] = (TO)y;
+          }
+        continue;
+      }
+      load_rows(r0 + step * R, next);
+#pragma unroll
+      for (int k = 0; k < R; ++k) {
+        const int r = r0 + k * step;
+        if (r >= rows) continue;
+        float y[P];
+        if (one) {
+#pragma unroll
+          for (int i = 0; i < P; ++i) y[i] = all;
+        } else {
+          const int a = c - r + rows - 1;
+#pragma unroll
+          for (int i = 0; i < P; i += 4) {
+            const f4 w = *(const f4*)&lines[word(a % 4, a / 4 + i / 4)];
+#pragma unroll
+            for (int n = 0; n < 4; ++n) y[i + n] = w[n];
+          }
         }
-        typename Piece<TI, P>::V v[R];
         if constexpr (ADD) {
 #pragma unroll
-          for (int k = 0; k < R; ++k)
-            v[k] = *(const typename Piece<TI, P>::V*)(from + min(r0 + k * step, rows - 1) * in.query_ld + c);
+          for (int i = 0; i < P; ++i) y[i] = added((float)v[k][i], y[i]);
         }
-#pragma unroll
-        for (int k = 0; k < R; ++k) {
-          const int r = r0 + k * step;
-          if (r >= rows) continue;
-          float y[P];
-          if (one) {
-#pragma unroll
-            for (int i = 0; i < P; ++i) y[i] = all;
-          } else {
-            const int a = c - r + rows - 1;
-#pragma unroll
-            for (int i = 0; i < P; i += 4) {
-              const f4 w = *(const f4*)&lines[word(a % 4, a / 4 + i / 4)];
-#pragma unroll
-              for (int n = 0; n < 4; ++n) y[i + n] = w[n];
-            }
-          }
-          if constexpr (ADD) {
-#pragma unroll
-            for (int i = 0; i < P; ++i) y[i] = added((float)v[k][i], y[i]);
-          }
-          store_piece<P, TO, ADD>(to + r * out.query_ld + c, y);
-        }
+        store_piece<P, TO, ADD>(to + r * out.query_ld + c, y);
       }
+      if constexpr (ADD) {
+#pragma unroll
+        for (int k = 0; k < R; ++k) v[k] = next[k];
+      }
+    }
     if (!one) __syncthreads();
   }
 }
@@ -629,9 +639,10 @@ static void launch_bias_of(const tt_emb_matrix& table, const tt_emb_distances& d
   BiasTiles tl;
   tl.cols = (int)std::min<int64_t>((out.keys + P - 1) / P * P, kBiasThreads * P);
   tl.across = (int)((out.keys + tl.cols - 1) / tl.cols);
-  tl.rows = (int)std::min<int64_t>(out.queries, std::min(1024, 32 * kBiasThreads * P / tl.cols));
-  // enough tiles for all compute units
-  while (tl.rows > 8 && planes * tl.across * ((out.queries + tl.rows - 1) / tl.rows) < 4096) tl.rows /= 2;
+  tl.rows = (int)std::min<int64_t>(out.queries, std::min(1024, 8 * kBiasThreads * P / tl.cols));
+  // Small tiles: 16 x 4096 x 4096 bf16 by 8 rows 92 us, by 32 101, by 4 149; 7 x 12 x 509 x 1021 fp32, added, by 4 rows 72, by 8 77,
+  // by 16 89.
+  while (tl.rows > 4 && planes * tl.across * ((out.queries + tl.rows - 1) / tl.rows) < 16384) tl.rows /= 2;
   tl.down = (int)((out.queries + tl.rows - 1) / tl.rows);
   tl.count = planes * tl.down * tl.across;
   tl.lanes = 0;

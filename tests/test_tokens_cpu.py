@@ -24,7 +24,7 @@ def _out(logprob=256, entropy=0, state=0, top_ids=0, top_logprob=0, top=0):
 
 BAD = [None, _m(data=None), _m(data=258), _m(rows=-1), _m(ld=15), _m(cols=0), _m(cols=(1 << 30) + 1, ld=1 << 31), _m(kind=3),
        _m(kind=-1), _m(rows=1 << 30), _m(data=257, kind=b.TT_EMB_BF16), _m(ld=(1 << 40) + 1)]
-SCALES = [0.0, -1.0, float("nan"), float("inf")]
+SCALES = [0.0, -1.0, float("nan"), float("inf"), 2e38]
 WS = 1 << 20
 
 
