@@ -106,19 +106,20 @@ struct BiasTiles {
   int rows, cols;  // of a tile
   int down, across;
   int64_t count;
-  int lanes;       // log2 of the threads side by side
   int line;        // places of a line: rows + cols and some more, a multiple of 8
+  bool in_place;
 };
 
-// A block takes a tile of one head.  Its diagonals' values come first, four copies of the line, each a place further, so that
-// any row finds its values in 16-byte words of one of them; a tile beyond the span has one value.  Where a thread takes two
-// words of them, those of even and odd number lie apart, so that the threads of a wavefront read side by side.
+// A block takes a tile of one head, whose pieces its threads take in turn, row by row.  Its diagonals' values come first, four
+// copies of the line, each a place further, so that any row finds its values in 16-byte words of one of them; a tile beyond the
+// span has one value.  Where a thread takes two words of them, those of even and odd number lie apart, so that the threads of a
+// wavefront read side by side.  A row's last piece starts early where it is cut off, and holds some of its neighbour's places.
 template <class TI, class TO, bool ADD>
 __global__ __launch_bounds__(kBiasThreads) void k_bias_tiles(tt_emb_matrix table, tt_emb_distances dist, float fill,
                                                              tt_emb_pairs in, tt_emb_pairs out, BiasTiles tl) {
   extern __shared__ __attribute__((aligned(16))) float lines[];
   constexpr int P = kBiasPiece<TI, TO, ADD>, R = kBiasAhead, kAhead = 4;
-  const int side = threadIdx.x & ((1 << tl.lanes) - 1), up = threadIdx.x >> tl.lanes, step = kBiasThreads >> tl.lanes;
+  typedef typename Piece<TI, P>::V V;
   auto word = [&](int copy, int w) {  // where the word's four values are
     return copy * tl.line + (P == 8 ? (w & 1) * (tl.line / 2) + w / 2 * 4 : w * 4);
   };
@@ -131,18 +132,33 @@ __global__ __launch_bounds__(kBiasThreads) void k_bias_tiles(tt_emb_matrix table
     const Values values{table, dist.bucket_of, dist.span, h, fill};
     const TI* from = (const TI*)in.data + (ADD ? b * in.batch_ld + h * in.head_ld + i0 * in.query_ld + j0 : 0);
     TO* to = (TO*)out.data + b * out.batch_ld + h * out.head_ld + i0 * out.query_ld + j0;
-    const int c = side * P;  // a tile is no wider than the block's threads
-    const bool whole = c + P <= cols;
-    typedef typename Piece<TI, P>::V V;
-    auto load_rows = [&](int r0, V(&v)[R]) {
-      if constexpr (ADD)
-        if (whole && r0 < rows) {
+    const uint32_t pieces = (uint32_t)(cols + P - 1) / P, down = kBiasThreads / pieces, right = kBiasThreads - down * pieces;
+    int row = (int)(threadIdx.x / pieces), piece = (int)(threadIdx.x - row * pieces);
+    struct Place {
+      int r, c, own;  // row, first column, and the first that is the piece's own
+    };
+    auto take = [&](Place(&p)[R]) {  // the thread's next pieces
 #pragma unroll
-          for (int k = 0; k < R; ++k) v[k] = *(const V*)(from + min(r0 + k * step, rows - 1) * in.query_ld + c);
+      for (int k = 0; k < R; ++k) {
+        p[k] = Place{row, max(min(piece * P, cols - P), 0), piece * P};
+        piece += (int)right;
+        row += (int)down + (piece >= (int)pieces);
+        piece -= piece >= (int)pieces ? (int)pieces : 0;
+      }
+    };
+    const bool wide = cols >= P;
+    auto load = [&](const Place(&p)[R], V(&v)[R]) {
+      if constexpr (ADD)
+        if (wide) {
+#pragma unroll
+          for (int k = 0; k < R; ++k)
+            if (p[k].r < rows) v[k] = *(const V*)(from + p[k].r * in.query_ld + p[k].c);
         }
     };
+    Place p[R], after[R];
     V v[R], next[R];
-    load_rows(up, v);
+    take(p);
+    load(p, v);
     const bool one = first >= dist.span || first + rows + cols - 2 <= -dist.span;
     float all = 0.f;
     if (one) {
@@ -162,28 +178,29 @@ __global__ __launch_bounds__(kBiasThreads) void k_bias_tiles(tt_emb_matrix table
       }
       __syncthreads();
     }
-    for (int r0 = up; r0 < rows && c < cols; r0 += step * R) {
-      if (!whole) {  // cut off
-        for (int r = r0; r < rows && r < r0 + step * R; r += step)
-          for (int i = c; i < cols; ++i) {
-            const int a = i - r + rows - 1;
-            float y = one ? all : lines[word(0, a / 4) + a % 4];
-            if constexpr (ADD) y = added((float)from[r * in.query_ld + i], y);
-            to[r * out.query_ld + i] = (TO)y;
-          }
-        continue;
-      }
-      load_rows(r0 + step * R, next);
+    while (p[0].r < rows) {
+      take(after);
+      load(after, next);
 #pragma unroll
       for (int k = 0; k < R; ++k) {
-        const int r = r0 + k * step;
-        if (r >= rows) continue;
+        if (p[k].r >= rows) continue;
+        const int a = p[k].c - p[k].r + rows - 1;  // the piece's first diagonal
+        TO* at = to + p[k].r * out.query_ld + p[k].c;
+        if (!wide) {  // a row shorter than a piece
+#pragma unroll
+          for (int i = 0; i < P; ++i) {
+            if (i >= cols) continue;
+            float y = one ? all : lines[word(0, (a + i) / 4) + (a + i) % 4];
+            if constexpr (ADD) y = added((float)from[p[k].r * in.query_ld + i], y);
+            at[i] = (TO)y;
+          }
+          continue;
+        }
         float y[P];
         if (one) {
 #pragma unroll
           for (int i = 0; i < P; ++i) y[i] = all;
         } else {
-          const int a = c - r + rows - 1;
 #pragma unroll
           for (int i = 0; i < P; i += 4) {
             const f4 w = *(const f4*)&lines[word(a % 4, a / 4 + i / 4)];
@@ -194,12 +211,19 @@ __global__ __launch_bounds__(kBiasThreads) void k_bias_tiles(tt_emb_matrix table
         if constexpr (ADD) {
 #pragma unroll
           for (int i = 0; i < P; ++i) y[i] = added((float)v[k][i], y[i]);
-        }
-        store_piece<P, TO, ADD>(to + r * out.query_ld + c, y);
-      }
-      if constexpr (ADD) {
+          if (tl.in_place && p[k].own != p[k].c) {  // what it read of its neighbour's may have the bias already
 #pragma unroll
-        for (int k = 0; k < R; ++k) v[k] = next[k];
+            for (int i = 0; i < P; ++i)
+              if (p[k].c + i >= p[k].own) at[i] = (TO)y[i];
+            continue;
+          }
+        }
+        store_piece<P, TO, ADD>(at, y);
+      }
+#pragma unroll
+      for (int k = 0; k < R; ++k) {
+        p[k] = after[k];
+        if constexpr (ADD) v[k] = next[k];
       }
     }
     if (!one) __syncthreads();
@@ -640,14 +664,15 @@ static void launch_bias_of(const tt_emb_matrix& table, const tt_emb_distances& d
   tl.cols = (int)std::min<int64_t>((out.keys + P - 1) / P * P, kBiasThreads * P);
   tl.across = (int)((out.keys + tl.cols - 1) / tl.cols);
   tl.rows = (int)std::min<int64_t>(out.queries, std::min(1024, 8 * kBiasThreads * P / tl.cols));
-  // Small tiles: 16 x 4096 x 4096 bf16 by 8 rows 92 us, by 32 101, by 4 149; 7 x 12 x 509 x 1021 fp32, added, by 4 rows 72, by 8 77,
-  // by 16 89.
-  while (tl.rows > 4 && planes * tl.across * ((out.queries + tl.rows - 1) / tl.rows) < 16384) tl.rows /= 2;
+  // Small tiles, of a batch of pieces for each thread: 16 x 4096 x 4096 bf16 by 8 rows 92 us, by 32 101, by 4 149; 7 x 12 x 509 x
+  // 1021 fp32, added, by 4 rows 72, by 8 77, by 16 89.
+  while (tl.rows * tl.cols > kBiasAhead * kBiasThreads * P &&
+         planes * tl.across * ((out.queries + tl.rows - 1) / tl.rows) < 16384)
+    tl.rows = (tl.rows + 1) / 2;
   tl.down = (int)((out.queries + tl.rows - 1) / tl.rows);
   tl.count = planes * tl.down * tl.across;
-  tl.lanes = 0;
-  while ((1 << tl.lanes) < kBiasThreads && (P << tl.lanes) < tl.cols) ++tl.lanes;
   tl.line = (tl.rows + tl.cols + 15) / 8 * 8;
+  tl.in_place = ADD && in.data == out.data;
   k_bias_tiles<TI, TO, ADD><<<(int)std::min(tl.count, kMostBlocks), kBiasThreads, 4 * tl.line * (int)sizeof(float), st>>>(
       table, dist, fill, in, out, tl);
 }
