@@ -664,8 +664,8 @@ static void launch_bias_of(const tt_emb_matrix& table, const tt_emb_distances& d
     return;
   }
   BiasTiles tl;
-  tl.cols = (int)std::min<int64_t>((out.keys + P - 1) / P * P, kBiasThreads * P);
-  tl.across = (int)((out.keys + tl.cols - 1) / tl.cols);
+  tl.across = (int)((out.keys + kBiasThreads * P - 1) / (kBiasThreads * P));
+  tl.cols = (int)(((out.keys + tl.across - 1) / tl.across + P - 1) / P * P);  // about the same width for all
   tl.rows = (int)std::min<int64_t>(out.queries, std::min(1024, 8 * kBiasThreads * P / tl.cols));
   // Small tiles, of a batch of pieces for each thread: 16 x 4096 x 4096 bf16 by 8 rows 92 us, by 32 101, by 4 149; 7 x 12 x 509 x
   // 1021 fp32, added, by 4 rows 72, by 8 77, by 16 89.

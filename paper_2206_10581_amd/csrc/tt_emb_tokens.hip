@@ -436,7 +436,6 @@ struct NarrowRow {
 };
 
 constexpr int kNarrowThreads = 256;
-constexpr int kNarrowList = 16;  // most lanes of a row whose list is made here; longer rows are taken by blocks
 template <int N>
 constexpr int kNarrowRows = N > 2 ? 1 : 4 / N;  // that a group of lanes has under way
 
@@ -477,34 +476,32 @@ __global__ __launch_bounds__(kNarrowThreads) void k_token_narrow(TokenRows t, To
     }
     const Sums s = o.entropy ? r.template sums<true>(t.cols, t.c) : r.template sums<false>(t.cols, t.c);
     if (lane == 0) put_numbers(o, t, row, s, at);
-    if constexpr (L <= kNarrowList) {
-      if (!o.top_ids) return;
-      // the largest that is left, `top` times: what is taken becomes 0
-      uint32_t left[N * P];
+    if (!o.top_ids) return;
+    // the largest that is left, `top` times: what is taken becomes 0
+    uint32_t left[N * P];
+#pragma unroll
+    for (int q = 0; q < N; ++q)
+#pragma unroll
+      for (int i = 0; i < P; ++i)
+        left[q * P + i] = r.mine(q, i, t.cols) ? (uint32_t)(key_of(r.x[q * P + i], 0) >> 32) : 0;
+    Key mine = 0;  // place k's, in lane k % L
+    for (int k = 0; k < o.top; ++k) {
+      uint32_t best = 0;
+#pragma unroll
+      for (int i = 0; i < N * P; ++i) best = max(best, left[i]);
+      const uint32_t most = lanes_of<L>(best, [](uint32_t a, uint32_t b) { return max(a, b); });
+      uint32_t place = INT_MAX;
+#pragma unroll
+      for (int q = N - 1; q >= 0; --q)
+#pragma unroll
+        for (int i = P - 1; i >= 0; --i) place = left[q * P + i] == most ? (uint32_t)(r.first[q] + i) : place;
+      place = lanes_of<L>(place, [](uint32_t a, uint32_t b) { return min(a, b); });
 #pragma unroll
       for (int q = 0; q < N; ++q)
 #pragma unroll
-        for (int i = 0; i < P; ++i)
-          left[q * P + i] = r.mine(q, i, t.cols) ? (uint32_t)(key_of(r.x[q * P + i], 0) >> 32) : 0;
-      Key mine = 0;  // place k's, in lane k % L
-      for (int k = 0; k < o.top; ++k) {
-        uint32_t best = 0;
-#pragma unroll
-        for (int i = 0; i < N * P; ++i) best = max(best, left[i]);
-        const uint32_t most = lanes_of<L>(best, [](uint32_t a, uint32_t b) { return max(a, b); });
-        uint32_t place = INT_MAX;
-#pragma unroll
-        for (int q = N - 1; q >= 0; --q)
-#pragma unroll
-          for (int i = P - 1; i >= 0; --i) place = left[q * P + i] == most ? (uint32_t)(r.first[q] + i) : place;
-        place = lanes_of<L>(place, [](uint32_t a, uint32_t b) { return min(a, b); });
-#pragma unroll
-        for (int q = 0; q < N; ++q)
-#pragma unroll
-          for (int i = 0; i < P; ++i) left[q * P + i] = r.first[q] + i == (int)place ? 0 : left[q * P + i];
-        if (lane == k % L) mine = most == 0 ? 0 : (Key)most << 32 | ~place;
-        if (k % L == L - 1 || k == o.top - 1) put_top(o, t, row, s, mine, lane <= k % L ? k / L * L + lane : o.top);
-      }
+        for (int i = 0; i < P; ++i) left[q * P + i] = r.first[q] + i == (int)place ? 0 : left[q * P + i];
+      if (lane == k % L) mine = most == 0 ? 0 : (Key)most << 32 | ~place;
+      if (k % L == L - 1 || k == o.top - 1) put_top(o, t, row, s, mine, lane <= k % L ? k / L * L + lane : o.top);
     }
   });
 }
@@ -825,13 +822,12 @@ static int grid_of(int64_t blocks) { return (int)std::min(blocks, kMostBlocks); 
 
 // Lanes and pieces of narrow rows: f(L, N) as constants; false: wider ones.
 template <class T, class F>
-static bool with_narrow(int cols, bool list, F&& f) {
+static bool with_narrow(int cols, F&& f) {
   constexpr int P = 16 / sizeof(T);
   if (cols <= 4 * P) f(std::integral_constant<int, 4>{}, std::integral_constant<int, 1>{});
   else if (cols <= 8 * P) f(std::integral_constant<int, 4>{}, std::integral_constant<int, 2>{});
   else if (cols <= 16 * P) f(std::integral_constant<int, 4>{}, std::integral_constant<int, 4>{});
   else if (cols <= 64 * P) f(std::integral_constant<int, 16>{}, std::integral_constant<int, 4>{});
-  else if (!list && cols <= 256 * P) f(std::integral_constant<int, 64>{}, std::integral_constant<int, 4>{});
   else return false;
   return true;
 }
@@ -859,17 +855,32 @@ static void launch_wide(const TokenRows& t, const TokenOut& o, const TokenParts&
 void launch_token_scores(const TokenRows& t, int type, const TokenOut& o, const TokenParts& parts, hipStream_t st) {
   with_type(type, [&](auto ti) {
     typedef decltype(ti) T;
-    // A long list of few rows is quicker made by blocks: 20 rows of 100 bf16 with 8, 16 and 64 places 9.3, 13.7 and 39.6 us
-    // narrow, 6.2, 7.8 and 8.6 by blocks; 3000 rows 9.6, 14.1 and 40 against 32, 43 and 48.
-    const bool by_blocks = o.top_ids != nullptr && o.top > 8 && t.rows <= 512 && t.cols * sizeof(T) >= 16;
-    const bool narrow = !by_blocks && with_narrow<T>(t.cols, o.top_ids != nullptr, [&](auto l, auto n) {
+    // A long list of few rows is quicker made by blocks: a narrow row's takes 0.6 us for each place, whatever the rows, a block's
+    // 3.5 ns for each row and 8 us.  20 rows of 100 bf16 with 16 and 64 places 13.7 and 39.6 us narrow, 7.8 and 8.6 by blocks; 100,000
+    // rows 46 and 131 against 350 and more.
+    const bool by_blocks = o.top_ids != nullptr && t.rows <= 160 * (o.top - 8) && t.cols * sizeof(T) >= 16;
+    const bool narrow = !by_blocks && with_narrow<T>(t.cols, [&](auto l, auto n) {
       constexpr int L = decltype(l)::value, N = decltype(n)::value, kSide = kNarrowThreads / L * kNarrowRows<N>;
       k_token_narrow<T, L, N><<<grid_of((t.rows + kSide - 1) / kSide), kNarrowThreads, 0, st>>>(t, o);
     });
     if (narrow) return;
-    // 4096 rows of 32,000 bf16 with entropy 33 us by blocks of 512 threads, 38 of 256; 48 of 128,000 with a list 25 and 21
-    if (o.top_ids) launch_wide<T, 256, true>(t, o, parts, st);
-    else launch_wide<T, 512, false>(t, o, parts, st);
+    // Threads of a block by the pieces of a row, of which a thread has four under way.  60M logits in all, us by 64 / 128 / 256 / 512
+    // threads: rows of 704 bf16 (88 pieces) 44 / 62 / 115, 1160 fp32 (290) 42 / 49 / 73, 3500 bf16 (438) 26 / 29 / 36, 5000 bf16
+    // (625) - / 27 / 33 / 50, 16,000 (2000) - / - / 28 / 27; 4096 rows of 32,000 - / - / 38 / 33.
+    // Lists: 20,000 rows of 2500 with 20 places 43 / 66 / 116, 3000 of 8000 21 / 21 / 25; 500 of 32,000 with 8 31 / 23 / 15.
+    const int64_t pieces = t.cols * (int64_t)sizeof(T) / 16;
+    if (o.top_ids) {
+      if (pieces <= 1024 && t.rows > 512) launch_wide<T, 64, true>(t, o, parts, st);
+      else launch_wide<T, 256, true>(t, o, parts, st);
+    } else if (pieces <= 512) {
+      launch_wide<T, 64, false>(t, o, parts, st);
+    } else if (pieces <= 1024) {
+      launch_wide<T, 128, false>(t, o, parts, st);
+    } else if (pieces <= 2048) {
+      launch_wide<T, 256, false>(t, o, parts, st);
+    } else {
+      launch_wide<T, 512, false>(t, o, parts, st);
+    }
   });
 }
 
@@ -910,12 +921,25 @@ void launch_token_loss(const TokenRows& t, int type, const float* weights, float
       typedef decltype(ti) T;
       typedef decltype(tout) TO;
       TO* to = (TO*)dx.data;
-      const bool narrow = with_narrow<T>(t.cols, false, [&](auto l, auto n) {
+      const bool narrow = with_narrow<T>(t.cols, [&](auto l, auto n) {
         constexpr int L = decltype(l)::value, N = decltype(n)::value, kSide = kNarrowThreads / L * kNarrowRows<N>;
         k_token_loss_narrow<T, TO, L, N><<<grid_of((t.rows + kSide - 1) / kSide), kNarrowThreads, 0, st>>>(
             t, weights, weight, logprob, to, dx.ld);
       });
-      if (!narrow) k_token_loss<T, TO, 1024><<<grid_of(t.rows), 1024, 0, st>>>(t, weights, weight, logprob, to, dx.ld);
+      if (narrow) return;
+      // 60M logits in all, us by 64 / 128 / 256 / 512 / 1024 threads: rows of 704 bf16 (88 pieces) 61 / 88 / 137, 3500 (438) 58 / 49 /
+      // 52, 5000 (625) - / - / 50 / 65 / 99, 16,000 (2000) - / - / 57 / 49 / 54, 32,000 (4000) - / - / 60 / 57 / 52; 4096 rows of
+      // 128,000 - / - / 605 / 486 / 442: of more rows at once the caches hold less until they are read again.
+      const int64_t pieces = t.cols * (int64_t)sizeof(T) / 16;
+      auto go = [&](auto nt) {
+        constexpr int NT = decltype(nt)::value;
+        k_token_loss<T, TO, NT><<<grid_of(t.rows), NT, 0, st>>>(t, weights, weight, logprob, to, dx.ld);
+      };
+      if (pieces <= 256) go(std::integral_constant<int, 64>{});
+      else if (pieces <= 512) go(std::integral_constant<int, 128>{});
+      else if (pieces <= 1024) go(std::integral_constant<int, 256>{});
+      else if (pieces <= 2048) go(std::integral_constant<int, 512>{});
+      else go(std::integral_constant<int, 1024>{});
     });
   });
 }
