@@ -427,9 +427,9 @@ int tt_emb_bias_workspace_bytes(const tt_emb_pairs* grad, int32_t span, size_t* 
  * Gradient of that with respect to the table:
  *   sum[u,h] = sum of grad[b,h,i,j] over all places (b,i,j) of bucket u
  *   add = 0   dtable = sum;   add = 1   dtable = dtable + sum
- * Places without a bucket are not read into any sum.  Sums are formed in fp32 over a few hundred places and in fp64 beyond, in a
- * fixed order, and rounded once.  workspace: device, 256-byte aligned; calls that share one must be ordered by a
- * stream.  May be captured into a HIP graph.
+ * Places without a bucket enter no sum, whatever they hold.  Sums are formed in fp32 within parts, of some rows of one sequence or
+ * of several, and in fp64 between parts, in an order that sizes and distances alone fix, and rounded once.  workspace: device,
+ * 256-byte aligned; calls that share one must be ordered by a stream.  May be captured into a HIP graph.
  */
 int tt_emb_bias_backward(const tt_emb_pairs* grad, const tt_emb_distances* distances, const tt_emb_matrix* dtable, int add,
                          void* workspace, size_t workspace_bytes, void* hip_stream);

@@ -1,7 +1,10 @@
 // Position bias of attention: a table [buckets, heads] looked up by the distance of a key from a query, alone or added to
 // scores, and its gradient, sums of the scores' gradients over all places of a bucket.
 //
-// A distance is j - i + o with one o for a sequence, so a head's bias has one value for every diagonal.
+// A distance is j - i + o with one o for a sequence, so a head's bias has one value for every diagonal.  Bound by the memory.
+// Measured (one MI355X, us a call among others): 16 x 4096 x 4096 bf16 written 91.8 (5.9 TB/s; a fill of that size into three
+// buffers in turn 78), 7 x 12 x 509 x 1021 fp32 added 68.6 (5.1 TB/s read and written), 64 x 16 x 1 x 4097 bf16 8.3 (the call);
+// sums of 8 x 16 x 2048 x 2048 bf16 206 (5.2 TB/s), of 3 x 12 x 129 x 515 fp32 18.5 (three launches).
 #include <algorithm>
 #include <type_traits>
 
@@ -60,7 +63,8 @@ constexpr int kBiasThreads = 256, kBiasAhead = 4;  // rows of a tile that a thre
 template <class TI, class TO, bool ADD>
 constexpr int kBiasPiece = 16 / (ADD && sizeof(TI) > sizeof(TO) ? sizeof(TI) : sizeof(TO));
 
-// Few queries: a block takes a row, a thread looks up its pieces' values; those beyond the span have one for all.
+// Few queries: a block takes a row, a thread looks up its pieces' values; those beyond the span have one for all.  64 x 16 x 1 x
+// 4097 bf16 7.7 us, with tiles 15.
 constexpr int kFewQueries = 4;
 template <class TI, class TO, bool ADD>
 __global__ __launch_bounds__(kBiasThreads) void k_bias_few(tt_emb_matrix table, tt_emb_distances dist, float fill,
@@ -112,8 +116,9 @@ struct BiasTiles {
 
 // A block takes a tile of one head, whose pieces its threads take in turn, row by row.  Its diagonals' values come first, four
 // copies of the line, each a place further, so that any row finds its values in 16-byte words of one of them; a tile beyond the
-// span has one value.  EVEN: all rows of all tiles are of whole pieces, and a block's threads take whole rows at once.  Where a thread takes two words of them, those of even and odd number lie apart, so that the threads of a
-// wavefront read side by side.  A row's last piece starts early where it is cut off, and holds some of its neighbour's places.
+// span has one value.  EVEN: all rows of all tiles are of whole pieces, and a block's threads take whole rows at once.  Where a
+// thread takes two words of them, those of even and odd number lie apart, so that the threads of a wavefront read side by side.  A
+// row's last piece starts early where it is cut off, and holds some of its neighbour's places.
 template <class TI, class TO, bool ADD, bool EVEN>
 __global__ __launch_bounds__(kBiasThreads) void k_bias_tiles(tt_emb_matrix table, tt_emb_distances dist, float fill,
                                                              tt_emb_pairs in, tt_emb_pairs out, BiasTiles tl) {
@@ -373,8 +378,10 @@ __device__ __forceinline__ float groups_sum(const T* p, int64_t ld, int from, in
 }
 
 // A block sums the diagonals of some rows of one head and of p.group sequences, a lane B of them at a time: its accumulators
-// stay, the row's place moves by a value from one row to the next.  All before the first and behind the last
-// diagonal are summed apart, row by row.
+// stay, the row's place moves by a value from one row to the next, so that loads need not be aligned, and nothing is exchanged
+// between lanes.  All before the first and behind the last diagonal are summed apart, row by row.  Bound by the memory where most
+// places are: 8 x 16 x 2048 x 2048 bf16 with 255 diagonals apart 194 us (5.5 TB/s).  A call, with the joins: 203, with the band in a
+// pass of its own 226, with a choice for every place 355.
 template <class T, int B>
 __global__ __launch_bounds__(kSumThreads) void k_bias_sums(tt_emb_pairs g, tt_emb_distances dist, int buckets, SumPlan p,
                                                            float* __restrict__ parts, PartReach* __restrict__ reach) {
@@ -739,6 +746,8 @@ void launch_bias_sums(const tt_emb_pairs& g, const tt_emb_distances& dist, const
     });
     distances_of(g, dist, &low, &count);
     const int blocks = (int)std::min<int64_t>((int64_t)(count + kWave - 1) / kWave * g.heads, kMostBlocks);
+    // Wavefronts of a block by the blocks, us by 4 / 16: 8 x 16 x 2048 x 2048 with 255 distances (64 blocks) 8.2 / 5.4, 2 x 8 x 512 x
+    // 512 with 255 4.4 / 4.8; with 4095 distances (1024 blocks) 10.5 / 15.8, 1 x 32 x 4096 x 4096 with 8191 (4096) 17 / 49.
     if (blocks >= 1024)
       k_bias_join<4><<<blocks, 4 * kWave, 0, st>>>(g.heads, low, count, p, ws.parts, ws.reach, ws.total, ws.reached);
     else
@@ -751,8 +760,11 @@ void launch_bias_sums(const tt_emb_pairs& g, const tt_emb_distances& dist, const
       k_bias_buckets<TO, W, U><<<(int)std::min(out.rows, kMostBlocks), W * kWave, 0, st>>>(
           g.heads, dist.bucket_of + dist.span + low, count, ws.total, ws.reached, (TO*)out.data, out.ld, (int)out.rows, add);
     };
-    if (count <= 1024) go(std::integral_constant<int, 4>{}, std::integral_constant<int, 4>{});
-    else if (out.rows >= 512) go(std::integral_constant<int, 4>{}, std::integral_constant<int, 16>{});
+    // Wavefronts of a bucket and distances ahead of each, us by 4 and 4 / 4 and 16 / 16 and 4: 255 distances in 32 buckets 5.8 / 8.0 /
+    // 6.0, 1023 in 200 5.9 / 7.7 / 5.3, in 300 5.3 / 7.2 / 6.2, 643 in 1001 4.1 / 6.4 / 8.2; 4095 in 32 12.9 / 11.9 / 5.6, 8191 in 64
+    // 24 / 22 / 9, in 600 18 / 16 / 14, in 8000 57 / 54 / 77.
+    if (count <= 1024 && out.rows >= 256) go(std::integral_constant<int, 4>{}, std::integral_constant<int, 4>{});
+    else if (out.rows >= 1024) go(std::integral_constant<int, 4>{}, std::integral_constant<int, 16>{});
     else go(std::integral_constant<int, 16>{}, std::integral_constant<int, 4>{});
   });
 }
