@@ -2,7 +2,7 @@
 // scores, and its gradient, sums of the scores' gradients over all places of a bucket.
 //
 // A distance is j - i + o with one o for a sequence, so a head's bias has one value for every diagonal.  Bound by the memory.
-// Measured (one MI355X, us a call among others): 16 x 4096 x 4096 bf16 written 91.8 (5.9 TB/s; a fill of that size into three
+// Measured (one MI355X, us a call among others): 16 x 4096 x 4096 bf16 written 86.5 (6.2 TB/s; a fill of that size into three
 // buffers in turn 78), 7 x 12 x 509 x 1021 fp32 added 68.6 (5.1 TB/s read and written), 64 x 16 x 1 x 4097 bf16 8.3 (the call);
 // sums of 8 x 16 x 2048 x 2048 bf16 206 (5.2 TB/s), of 3 x 12 x 129 x 515 fp32 18.5 (three launches).
 #include <algorithm>
@@ -671,11 +671,16 @@ static void launch_bias_of(const tt_emb_matrix& table, const tt_emb_distances& d
     return;
   }
   BiasTiles tl;
-  tl.across = (int)((out.keys + kBiasThreads * P - 1) / (kBiasThreads * P));
+  // Pieces of a tile's rows: a tile of as many places has fewer diagonals where its sides are alike, and more tiles lie beyond the
+  // span.  us by 64 / 128 / 256: 16 x 4096 x 4096 bf16 86 / 95 / 93, with a span over all of it 83 / 92 / 132, added 181 / 182 / 194,
+  // 16 x 2048 x 4096 fp32 84 / 88 / 95; but of rows that are no whole tiles, 16 x 2000 x 4000 bf16 65 / 64 / 96, x 4001 87 / 64 /
+  // 98, fp32 154 / 126 / 98, added 229 / 218 / 212.
+  const int wide = (out.keys % (kWave * P) == 0 ? 1 : P == 8 ? 2 : 4) * kWave * P;
+  tl.across = (int)((out.keys + wide - 1) / wide);
   tl.cols = (int)(((out.keys + tl.across - 1) / tl.across + P - 1) / P * P);  // about the same width for all
   tl.rows = (int)std::min<int64_t>(out.queries, std::min(1024, 8 * kBiasThreads * P / tl.cols));
-  // Small tiles, of a batch of pieces for each thread: 16 x 4096 x 4096 bf16 by 8 rows 92 us, by 32 101, by 4 149; 7 x 12 x 509 x
-  // 1021 fp32, added, by 4 rows 72, by 8 77, by 16 89.
+  // Small tiles, of a batch of pieces for each thread: 7 x 12 x 509 x 1021 fp32, added, by 4 rows 72 us, by 8 77, by 16 89; 16 x 4096
+  // x 4096 bf16 by tiles of 2048 columns and 8 rows 92, 32 rows 101, 4 rows 149.
   while (tl.rows * tl.cols > kBiasAhead * kBiasThreads * P &&
          planes * tl.across * ((out.queries + tl.rows - 1) / tl.rows) < 16384)
     tl.rows = (tl.rows + 1) / 2;
@@ -684,7 +689,7 @@ static void launch_bias_of(const tt_emb_matrix& table, const tt_emb_distances& d
   tl.line = (tl.rows + tl.cols + 15) / 8 * 8;
   tl.in_place = ADD && in.data == out.data;
   const int blocks = (int)std::min(tl.count, kMostBlocks), lds = 4 * tl.line * (int)sizeof(float);
-  // Whole pieces: written alone 101 to 91 us at 16 x 4096 x 4096 bf16, but added 203 to 233.
+  // Whole pieces: written alone 101 to 91 us at 16 x 4096 x 4096 bf16 by tiles of 2048 columns, but added 203 to 233.
   if constexpr (!ADD)
     if (out.keys % tl.cols == 0 && kBiasThreads * P % tl.cols == 0) {
       k_bias_tiles<TI, TO, ADD, true><<<blocks, kBiasThreads, lds, st>>>(table, dist, fill, in, out, tl);

@@ -63,7 +63,8 @@ def _buckets(of, offset, batch, queries, keys):
 
 MAPS = ["both", "causal", "far", "each", "one", "mixed", "none"]
 # batch, heads, queries, keys
-SIZES = [(1, 1, 1, 1), (3, 2, 1, 300), (2, 3, 40, 1), (2, 3, 17, 33), (1, 2, 129, 515), (2, 1, 300, 1100), (5, 2, 64, 64), (1, 3, 7, 2051)]
+SIZES = [(1, 1, 1, 1), (3, 2, 1, 300), (2, 3, 40, 1), (2, 3, 17, 33), (1, 2, 129, 515), (2, 1, 300, 1100), (5, 2, 64, 64), (1, 3, 7, 2051),
+         (1, 2, 70, 1024), (1, 1, 40, 2000)]
 
 
 # many heads, so that a part holds several sequences; short rows; many buckets
