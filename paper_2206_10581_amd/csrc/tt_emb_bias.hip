@@ -597,7 +597,8 @@ __global__ __launch_bounds__(W * kWave) void k_bias_buckets(int heads, const int
   __shared__ double sums[kThreads];  // of heads h0, h0 + 1, ...
   static_assert(U * W <= kWave, "a count for each lane");
   const int lane = threadIdx.x % kWave, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
-  for (int u = blockIdx.x; u < buckets; u += gridDim.x)
+  for (int64_t at_u = blockIdx.x; at_u < buckets; at_u += gridDim.x) {  // in 64 bits: the step may lead beyond 2^31
+    const int u = (int)at_u;
     for (int h0 = 0; h0 < heads; h0 += kThreads) {
       sums[threadIdx.x] = 0.0;
       for (int r0 = 0; r0 < count; r0 += U * kThreads) {
@@ -653,6 +654,7 @@ __global__ __launch_bounds__(W * kWave) void k_bias_buckets(int heads, const int
         *to = (TO)(float)(add ? (double)(float)*to + sums[threadIdx.x] : sums[threadIdx.x]);
       }
     }
+  }
 }
 
 // ---------------------------------------------------------------------------------------------
