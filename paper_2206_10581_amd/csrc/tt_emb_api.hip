@@ -1047,6 +1047,56 @@ static bool good_pairs(const tt_emb_pairs* p) {
   return good_sizes(p) && known_type(p->type) && step(p->batch_ld) && step(p->head_ld) && step(p->query_ld) &&
          (no_pairs(*p) || p->data != nullptr) && ((uintptr_t)p->data & (type_bytes(p->type) - 1)) == 0;
 }
+// Whether two arrays of the same sizes (of at least one pair) are the same one, or share no byte.  Of two with different strides
+// or sizes of types, or whose own places overlap, the whole ranges count.
+static bool same_or_apart(const tt_emb_pairs& a, const tt_emb_pairs& b) {
+  struct Axis {
+    int64_t step, other, more;  // strides of both, and how many places follow the first
+  };
+  Axis axes[] = {{a.batch_ld, b.batch_ld, a.batch - 1},
+                 {a.head_ld, b.head_ld, a.heads - 1},
+                 {a.query_ld, b.query_ld, a.queries - 1},
+                 {1, 1, a.keys - 1}};
+  typedef __int128 Wide;  // a stride of 2^40 times 2^30 places
+  const int sa = type_size(a.type), sb = type_size(b.type);
+  bool alike = sa == sb;
+  Wide la = 0, lb = 0;  // the last place
+  for (Axis& x : axes) {
+    if (x.more == 0) x.step = x.other = 0;  // says nothing
+    alike = alike && x.step == x.other;
+    la += (Wide)x.more * x.step;
+    lb += (Wide)x.more * x.other;
+  }
+  if (a.data == b.data && a.type == b.type && alike) return true;
+  const Wide at = (Wide)(uintptr_t)b.data - (Wide)(uintptr_t)a.data;
+  if (at >= (la + 1) * sa || -at >= (lb + 1) * sb) return true;
+  if (!alike) return false;
+  std::sort(axes, axes + 4, [](const Axis& x, const Axis& y) { return x.step > y.step; });
+  // Whether sums of d * step, |d| <= more, reach from a's first place to b's: where a step is longer than all shorter ones together,
+  // one of two multiples of it leaves what these can reach.
+  Wide reached[16] = {at / sa}, left = la;
+  int n = 1;
+  for (const Axis& x : axes) {
+    if (x.more == 0) continue;
+    left -= (Wide)x.more * x.step;
+    if (x.step <= left) return false;
+    int m = 0;
+    Wide next[16];
+    for (int k = 0; k < n; ++k) {
+      Wide d = reached[k] / x.step;
+      if (reached[k] % x.step < 0) --d;
+      for (int up = 0; up < 2; ++up, ++d) {
+        const Wide rest = reached[k] - d * x.step;
+        if (d <= x.more && -d <= x.more && rest <= left && -rest <= left) next[m++] = rest;
+      }
+    }
+    std::copy(next, next + m, reached);
+    n = m;
+  }
+  for (int k = 0; k < n; ++k)
+    if (reached[k] == 0) return false;
+  return true;
+}
 static bool good_distances(const tt_emb_distances* d) {
   return d != nullptr && d->bucket_of != nullptr && ((uintptr_t)d->bucket_of & 3u) == 0 && ((uintptr_t)d->offsets & 7u) == 0 &&
          d->span >= 0 && d->span <= 1 << 20;
@@ -1447,6 +1497,7 @@ int tt_emb_bias_forward(const tt_emb_matrix* table, const tt_emb_distances* dist
                         in->queries != out->queries || in->keys != out->keys))
     return TT_EMB_EINVAL;
   if (no_pairs(*out)) return TT_EMB_OK;
+  if (in != nullptr && !same_or_apart(*in, *out)) return TT_EMB_EINVAL;
   launch_bias(*table, *distances, fill, in, *out, (hipStream_t)hip_stream);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? TT_EMB_OK : hip_fail(e);
