@@ -545,6 +545,13 @@ class _OnDevice:
             raise ValueError(f"strides {t.stride()}: values of a row side by side, rows that do not overlap needed")
         return TTEmbMatrix(t.data_ptr(), rows, step if rows > 1 else cols, cols, self._type(t))
 
+    def _capturing(self):
+        cuda = self.torch.cuda
+        if cuda.current_device() == self.index:
+            return cuda.is_current_stream_capturing()
+        with cuda.device(self.index):
+            return cuda.is_current_stream_capturing()
+
     def _make_workspace(self, nbytes):
         self._home = self._stream(self.index)  # the workspace belongs to this stream
         self.workspace = self.torch.empty(nbytes + 256, dtype=self.torch.uint8, device=self.device)
@@ -990,9 +997,10 @@ class PositionBias(_OnDevice):
         rc, nbytes = tt_emb_bias_workspace_bytes(g, d.span)
         if rc:
             raise TTEmbError(rc, "tt_emb_bias_workspace_bytes")
-        if nbytes > self.workspace_bytes:
-            self._make_workspace(nbytes)
-            self._spaces.append(self.workspace)  # a captured graph may go on using a smaller one
+        if nbytes > self.workspace_bytes:  # sizes that rise in small steps do not make one each
+            self._make_workspace(max(nbytes, self.workspace_bytes * 3 // 2))
+        if self._capturing() and not any(space is self.workspace for space in self._spaces):
+            self._spaces.append(self.workspace)  # the graph goes on using it when a larger one has been made
         self._call(self.lib.tt_emb_bias_backward, byref(g), byref(d), byref(self._matrix(out)), 1 if add else 0, self._ws_ptr,
                    self.workspace_bytes)
         return out
