@@ -585,6 +585,21 @@ __global__ __launch_bounds__(W * kWave) void k_bias_join(int heads, int low, int
   }
 }
 
+// A sum in fp64 as a value of a table, rounded once: on the way to 16 bits fp32 holds it cut off towards zero, its last bit set where
+// something was cut off, so that no such value lies halfway between two of 16 bits.
+template <class T>
+__device__ __forceinline__ T rounded_once(double x) {
+  float f = (float)x;
+  if constexpr (sizeof(T) < sizeof(float)) {
+    const double back = (double)f;
+    if (back != x && x == x) {
+      const uint32_t b = __builtin_bit_cast(uint32_t, f);
+      f = __builtin_bit_cast(float, (fabs(back) > fabs(x) ? b - 1 : b) | 1u);
+    }
+  }
+  return (T)f;
+}
+
 // A block adds up the distances of one bucket in all heads: W * 64 * U at a time, first which they are, in order, then their
 // totals, of few by a thread for each head, of more by a wavefront.
 constexpr int kFewDistances = 16;
@@ -651,7 +666,7 @@ __global__ __launch_bounds__(W * kWave) void k_bias_buckets(int heads, const int
       const int h = h0 + (int)threadIdx.x;
       if (h < heads) {
         TO* to = out + u * ld + h;
-        *to = (TO)(float)(add ? (double)(float)*to + sums[threadIdx.x] : sums[threadIdx.x]);
+        *to = rounded_once<TO>(add ? (double)(float)*to + sums[threadIdx.x] : sums[threadIdx.x]);
       }
     }
   }
