@@ -348,7 +348,7 @@ typedef struct {
   int32_t unused;
 } tt_emb_token_out;
 
-/* Bytes of workspace that tt_emb_token_scores and tt_emb_token_loss need, the same for all sizes. */
+/* Bytes of workspace that tt_emb_token_scores needs and tt_emb_token_loss asks for, the same for all sizes. */
 int tt_emb_token_workspace_bytes(size_t* bytes);
 
 /*
@@ -379,8 +379,9 @@ int tt_emb_token_backward(const tt_emb_matrix* logits, const int64_t* tokens, fl
 
 /*
  * Both for a loss that is known beforehand, -sum_b w_b * logprob[b]: writes logprob (device fp32[rows]) and the
- * loss's gradient with respect to the logits.  w_b = weight * weights[b] (device fp32[rows], null: 1), weight finite.  dlogits and
- * workspace as above.
+ * loss's gradient with respect to the logits.  w_b = weight * weights[b] (device fp32[rows], null: 1), weight finite.  dlogits as
+ * above.  workspace: checked as in tt_emb_token_scores and reserved; a row is summed by the block that writes its gradient, and
+ * nothing is stored there.
  */
 int tt_emb_token_loss(const tt_emb_matrix* logits, const int64_t* tokens, float scale, const float* weights, float weight,
                       float* logprob, const tt_emb_matrix* dlogits, void* workspace, size_t workspace_bytes,
@@ -429,7 +430,9 @@ int tt_emb_bias_workspace_bytes(const tt_emb_pairs* grad, int32_t span, size_t* 
  *   sum[u,h] = sum of grad[b,h,i,j] over all places (b,i,j) of bucket u
  *   add = 0   dtable = sum;   add = 1   dtable = dtable + sum
  * Places without a bucket enter no sum, whatever they hold.  Sums are formed in fp32 within parts, of some rows of one sequence or
- * of several, and in fp64 between parts, in an order that sizes and distances alone fix, and rounded once.  workspace: device,
+ * of several, and in fp64 between parts, in an order that sizes and distances alone fix, and rounded once, to 16 bits too.  Every
+ * bucket looks through all distances that may occur (with offsets: all 2 * span + 1), so that part's time grows with buckets times
+ * distances: 65,537 of each take 2.8 ms, a bucket for each of 2^21 distances would take seconds.  workspace: device,
  * 256-byte aligned; calls that share one must be ordered by a stream.  May be captured into a HIP graph.
  */
 int tt_emb_bias_backward(const tt_emb_pairs* grad, const tt_emb_distances* distances, const tt_emb_matrix* dtable, int add,

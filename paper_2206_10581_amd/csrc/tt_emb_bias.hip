@@ -3,8 +3,8 @@
 //
 // A distance is j - i + o with one o for a sequence, so a head's bias has one value for every diagonal.  Bound by the memory.
 // Measured (one MI355X, us a call among others): 16 x 4096 x 4096 bf16 written 86.5 (6.2 TB/s; a fill of that size into three
-// buffers in turn 78), 7 x 12 x 509 x 1021 fp32 added 68.6 (5.1 TB/s read and written), 64 x 16 x 1 x 4097 bf16 8.3 (the call);
-// sums of 8 x 16 x 2048 x 2048 bf16 206 (5.2 TB/s), of 3 x 12 x 129 x 515 fp32 18.5 (three launches).
+// buffers in turn 78), 7 x 12 x 509 x 1021 fp32 added 68.6 (5.1 TB/s read and written), 64 x 16 x 1 x 4097 bf16 8.8 (the call);
+// sums of 8 x 16 x 2048 x 2048 bf16 206 (5.2 TB/s), of 3 x 12 x 129 x 515 fp32 18.8 (three launches).
 #include <algorithm>
 #include <type_traits>
 
@@ -585,8 +585,8 @@ __global__ __launch_bounds__(W * kWave) void k_bias_join(int heads, int low, int
   }
 }
 
-// A sum in fp64 as a value of a table, rounded once: on the way to 16 bits fp32 holds it cut off towards zero, its last bit set where
-// something was cut off, so that no such value lies halfway between two of 16 bits.
+// A sum in fp64 as a value of a table, rounded once: on the way to 16 bits fp32 holds it cut off towards zero, its last bit set
+// where something was cut off, so that no such value lies halfway between two of 16 bits.
 template <class T>
 __device__ __forceinline__ T rounded_once(double x) {
   float f = (float)x;
@@ -601,7 +601,9 @@ __device__ __forceinline__ T rounded_once(double x) {
 }
 
 // A block adds up the distances of one bucket in all heads: W * 64 * U at a time, first which they are, in order, then their
-// totals, of few by a thread for each head, of more by a wavefront.
+// totals, of few by a thread for each head, of more by a wavefront.  Every bucket looks at all distances, and one block has all
+// of the bucket that holds what is far: with long spans and offsets the joins and this kernel are most of a call (10 x 30 x 11 x 1211
+// fp16 with a span of 17,004: sums 13 us, joins 32, 16 buckets 21), and 65,537 buckets of a distance each take 2.8 ms.
 constexpr int kFewDistances = 16;
 template <class TO, int W, int U>
 __global__ __launch_bounds__(W * kWave) void k_bias_buckets(int heads, const int32_t* __restrict__ bucket_of, int count,
