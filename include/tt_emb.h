@@ -415,8 +415,8 @@ typedef struct {
  * out[b,h,i,j] = in[b,h,i,j] + table[bucket,h] for the bucket of (b,i,j), or without `in` the second term alone; where there is no
  * bucket, `fill` (-infinity: a mask) stands for the table's value.  An infinite value of table or fill replaces in's,
  * whatever that holds.  table: [buckets][heads], heads up to 65536.  in: sizes as out; may be out itself (same address, type and
- * strides) and overlaps it no other way: what does is refused, and so is, within out's range, an array of other strides or of a
- * type of another size.  Any types; sums in fp32, rounded once.  May be captured into a HIP graph.
+ * strides) and overlaps it no other way: what does is refused, and so is, within out's range, an array of other pitches in
+ * bytes.  Any types; sums in fp32, rounded once.  May be captured into a HIP graph.
  */
 int tt_emb_bias_forward(const tt_emb_matrix* table, const tt_emb_distances* distances, float fill,
                         const tt_emb_pairs* in, const tt_emb_pairs* out, void* hip_stream);

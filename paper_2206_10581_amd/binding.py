@@ -972,7 +972,7 @@ class PositionBias(_OnDevice):
 
     def add_to(self, scores, offset=0, out=None):
         """scores + bias, in out, or (None) in place.  out: the scores themselves, or a tensor that shares no memory with them; within
-        their range it has the same strides (columns or rows beside theirs in one buffer)."""
+        their range it has the same pitches in bytes (columns or rows beside theirs in one buffer)."""
         if out is None:
             out = scores
         elif out.shape != scores.shape:

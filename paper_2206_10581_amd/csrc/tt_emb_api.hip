@@ -1047,54 +1047,52 @@ static bool good_pairs(const tt_emb_pairs* p) {
   return good_sizes(p) && known_type(p->type) && step(p->batch_ld) && step(p->head_ld) && step(p->query_ld) &&
          (no_pairs(*p) || p->data != nullptr) && ((uintptr_t)p->data & (type_bytes(p->type) - 1)) == 0;
 }
-// Whether two arrays of the same sizes (of at least one pair) are the same one, or share no byte.  Of two with different strides
-// or sizes of types, or whose own places overlap, the whole ranges count.
+// Whether two arrays of the same sizes (of at least one pair) are the same one, or share no byte.  Of two with different pitches, or
+// whose own rows overlap, the whole ranges count.
 static bool same_or_apart(const tt_emb_pairs& a, const tt_emb_pairs& b) {
-  struct Axis {
-    int64_t step, other, more;  // strides of both, and how many places follow the first
-  };
-  Axis axes[] = {{a.batch_ld, b.batch_ld, a.batch - 1},
-                 {a.head_ld, b.head_ld, a.heads - 1},
-                 {a.query_ld, b.query_ld, a.queries - 1},
-                 {1, 1, a.keys - 1}};
   typedef __int128 Wide;  // a stride of 2^40 times 2^30 places
-  const int sa = type_size(a.type), sb = type_size(b.type);
-  bool alike = sa == sb;
-  Wide la = 0, lb = 0;  // the last place
+  const Wide sa = type_size(a.type), sb = type_size(b.type), wa = a.keys * sa, wb = b.keys * sb;
+  struct Axis {
+    Wide pitch, other;  // of both, in bytes
+    int64_t more;       // how many places follow the first
+  };
+  Axis axes[] = {{a.batch_ld * sa, b.batch_ld * sb, a.batch - 1},
+                 {a.head_ld * sa, b.head_ld * sb, a.heads - 1},
+                 {a.query_ld * sa, b.query_ld * sb, a.queries - 1}};
+  bool alike = true;
+  Wide la = 0, lb = 0;  // where the last row starts
   for (Axis& x : axes) {
-    if (x.more == 0) x.step = x.other = 0;  // says nothing
-    alike = alike && x.step == x.other;
-    la += (Wide)x.more * x.step;
-    lb += (Wide)x.more * x.other;
+    if (x.more == 0) x.pitch = x.other = 0;  // says nothing
+    alike = alike && x.pitch == x.other;
+    la += x.more * x.pitch;
+    lb += x.more * x.other;
   }
   if (a.data == b.data && a.type == b.type && alike) return true;
   const Wide at = (Wide)(uintptr_t)b.data - (Wide)(uintptr_t)a.data;
-  if (at >= (la + 1) * sa || -at >= (lb + 1) * sb) return true;
+  if (at >= la + wa || -at >= lb + wb) return true;
   if (!alike) return false;
-  std::sort(axes, axes + 4, [](const Axis& x, const Axis& y) { return x.step > y.step; });
-  // Whether sums of d * step, |d| <= more, reach from a's first place to b's: where a step is longer than all shorter ones together,
-  // one of two multiples of it leaves what these can reach.
-  Wide reached[16] = {at / sa}, left = la;
+  std::sort(axes, axes + 3, [](const Axis& x, const Axis& y) { return x.pitch > y.pitch; });
+  // Whether sums of d * pitch, |d| <= more, lead from a row of a to one of b that it meets.  Where a pitch holds all that the shorter
+  // ones reach and a row, only two multiples of it come near enough.
+  Wide rests[8] = {at}, left = la;
   int n = 1;
   for (const Axis& x : axes) {
     if (x.more == 0) continue;
-    left -= (Wide)x.more * x.step;
-    if (x.step <= left) return false;
+    left -= x.more * x.pitch;
+    if (x.pitch < left + std::max(wa, wb)) return false;
     int m = 0;
-    Wide next[16];
+    Wide next[8];
     for (int k = 0; k < n; ++k) {
-      Wide d = reached[k] / x.step;
-      if (reached[k] % x.step < 0) --d;
-      for (int up = 0; up < 2; ++up, ++d) {
-        const Wide rest = reached[k] - d * x.step;
-        if (d <= x.more && -d <= x.more && rest <= left && -rest <= left) next[m++] = rest;
-      }
+      Wide d = rests[k] / x.pitch;
+      if (rests[k] % x.pitch < 0) --d;
+      for (int up = 0; up < 2; ++up, ++d)
+        if (d <= x.more && -d <= x.more) next[m++] = rests[k] - d * x.pitch;
     }
-    std::copy(next, next + m, reached);
+    std::copy(next, next + m, rests);
     n = m;
   }
   for (int k = 0; k < n; ++k)
-    if (reached[k] == 0) return false;
+    if (rests[k] < wa && -rests[k] < wb) return false;
   return true;
 }
 static bool good_distances(const tt_emb_distances* d) {

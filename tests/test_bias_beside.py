@@ -38,6 +38,22 @@ def test_beside_each_other_in_one_buffer():
         assert torch.equal(room[~where], before[~where])
 
 
+def test_beside_each_other_in_two_types():
+    """Scores in fp32 and an output in bf16, in rows of one buffer, on either side."""
+    import torch
+    import paper_2206_10581_amd as tt
+    bias = _made()
+    room = _room(2, 3, 9, 90)
+    for scores, out in ((room[..., :50], room.view(torch.bfloat16)[..., 100:150]),
+                        (room[..., 25:75], room.view(torch.bfloat16)[..., :50])):
+        given = scores.clone()
+        want = bias.add_to(given, -4, out=torch.empty(out.shape, dtype=torch.bfloat16, device="cuda"))
+        assert torch.equal(bias.add_to(scores, -4, out=out), want) and torch.equal(scores, given)
+    for first in (99, 49):                                     # a place too early
+        with pytest.raises(tt.TTEmbError):
+            bias.add_to(room[..., :50], out=room.view(torch.bfloat16)[..., first:first + 50])
+
+
 def test_over_the_scores():
     import torch
     bias, x = _made(), _room(2, 3, 9, 50)
